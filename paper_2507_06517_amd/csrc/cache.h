@@ -106,7 +106,7 @@ struct Code<SPINDLE_I8> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int c = (int8_t)(w >> (8 * i));
-      const float t = (float)c * f;
+      const float t = c ? (float)c * f : 0.f;                         // (f overflows where zeros alone go to the smallest scale)
       float r = __builtin_rintf(t);
       if (__builtin_fabsf(__builtin_fabsf(t - r) - 0.5f) < 1e-4f) r = (float)__builtin_rint((double)c * (double)from / (double)to);
       o |= ((uint32_t)(int)__builtin_amdgcn_fmed3f(r, -127.f, 127.f) & 0xFFu) << (8 * i);

@@ -581,3 +581,24 @@ def test_example_serves_from_the_cache(sb):
     # the same text through integers: the codes' steps are all that differs
     other = ex.serve(prompt=700, budget=200, branches=3, steps=4, fmt="i8")[0].float()
     assert (other[0] - out[0].float()).abs().max() < 0.25
+
+
+# ------------------------------------------------------------------ compaction at the ends of the numbers
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_compact_of_zeros_from_pages_of_large_values(sb, fmt):
+    """A new page whose kept tokens are zeros (zero vectors, NaN stored as zeros) has the smallest scale, and its pages' scales
+    over that one are no number."""
+    rng = np.random.default_rng(73)
+    x = tokens(rng, 128, 2) * np.float32(1e4)
+    x[40:50], x[100:110] = 0, np.nan
+    cache = sb.new_cache(4, 2, 64, fmt)
+    table, out = np.int32([[1, 3]]), np.int32([[2]])
+    sb.cache_append(cache, dev(table), dev(np.int32([0])), dev(x), dev(x[::-1]), cu_new=dev(np.int32([0, 128])), max_new=128)
+    zeros = np.r_[40:50, 100:110]                                     # of K; mirrored ones of V
+    kept = np.int32([[zeros, np.r_[0:20]]])
+    want = pools_of(cache)
+    sb.cache_compact(cache, dev(table), dev(np.int32([128])), dev(kept), dev(np.int32([20])), dev(out))
+    ref.compact(want, table, [128], kept, [20], out)
+    same_pools(cache, want)
+    assert (cache.k[2, 0] == 0).all() and cache.k_scale[2, 0].item() == ref.TINY and cache.v_scale[2, 0].item() > 1
