@@ -1,4 +1,6 @@
 // The paged cache in 8 bits: quantising new tokens into it, gathering kept tokens into fewer pages, copying pages.
+#include <float.h>
+
 #include "cache.h"
 
 namespace spindle {
@@ -197,7 +199,7 @@ __global__ void cache_compact(CompactArgs a) {
     amax = fmaxf(amax, Code<FMT>::magnitude(max(Code<FMT>::largest4(w[i][0]), Code<FMT>::largest4(w[i][1]))) * from[i]);
   }
   amax = block_max(amax, part);
-  const float s = Code<FMT>::scale_for(amax);
+  const float s = Code<FMT>::scale_for(fminf(amax, FLT_MAX));        // (127 times a rounded scale may lie above the largest number)
   const size_t row0 = page_row(c, page, head);
   uint8_t *out = (is_v ? c.v : c.k) + row0 * kHeadDim;
 #pragma unroll

@@ -602,3 +602,18 @@ def test_compact_of_zeros_from_pages_of_large_values(sb, fmt):
     ref.compact(want, table, [128], kept, [20], out)
     same_pools(cache, want)
     assert (cache.k[2, 0] == 0).all() and cache.k_scale[2, 0].item() == ref.TINY and cache.v_scale[2, 0].item() > 1
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_compact_of_the_largest_numbers(sb, fmt):
+    """127 times a scale made of the largest number is none any more; the scale of the new page has to stay one."""
+    rng = np.random.default_rng(79)
+    x = tokens(rng, 64, 1)
+    x[5, 0, 7], x[6, 0, 8] = np.finfo(np.float32).max, -np.finfo(np.float32).max
+    cache = sb.new_cache(2, 1, 64, fmt)
+    sb.cache_append(cache, dev(np.int32([[1]])), dev(np.int32([0])), dev(x), dev(-x), cu_new=dev(np.int32([0, 64])), max_new=64)
+    sb.cache_compact(cache, dev(np.int32([[1]])), dev(np.int32([64])), dev(np.arange(64, dtype=np.int32).reshape(1, 1, 64)), dev(np.int32([64])),
+                     dev(np.int32([[0]])))
+    for codes, scale in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
+        assert torch.equal(codes[0], codes[1]) and torch.equal(scale[0], scale[1])
+        assert torch.isfinite(scale).all() and (codes[0, 0, 5:7, 7:9] != 0).any()
