@@ -748,8 +748,9 @@ def cache_append(cache: Cache, table, lens, K, V, cu_new=None, max_new=None, pos
 
 def cache_attend(cache: Cache, table, lens, Q, group_size, cu_q=None, max_q=None, scale=None, softcap=0.0, slopes=None, prefix=None,
                  q_pos=None, want_lse=False, out=None, lse=None, workspace=None):
-    """Attention of the newest tokens (stored already, lens [B] counts them) over their sequences.  Q [B, m, H * group, d], or,
-    with cu_q [B + 1] int32, [tokens of all, H * group, d] and max_q.  Returns out, or (out, lse) with want_lse; out, lse and
+    """Attention of the newest tokens (stored already, lens [B] counts them) over their sequences.  Q [B, m, H * group, d]
+    (the tokens of all sequences at one stride), or, with cu_q [B + 1] int32, [tokens of all, H * group, d] and max_q, the most tokens
+    of one sequence.  Returns out, or (out, lse) with want_lse; out, lse and
     workspace may be passed in (a workspace of spindle_attend_workspace_bytes)."""
     B, width = _check_table(cache, table, lens)
     dev, hq, shape, strides = cache.device, cache.n_kv_heads * group_size, Q.shape, Q.stride()
@@ -759,12 +760,17 @@ def cache_attend(cache: Cache, table, lens, Q, group_size, cu_q=None, max_q=None
         if shape[0] != B:
             raise ValueError(f"Q has {shape[0]} sequences, table {B}")
         max_q, total = shape[1], B * shape[1]
-        if B > 1 and strides[0] != max_q * strides[1]:
+        st = strides[0 if max_q == 1 else 1]       # (with one token a sequence the next token is the next sequence's)
+        if max_q > 1 and B > 1 and strides[0] != max_q * st:
             raise ValueError("the tokens of all sequences must follow each other at one stride")
     else:
         _ints(cu_q, "cu_q", (B + 1,), dev)
-        total = shape[0]
+        total, st = shape[0], strides[0]
         max_q = total if max_q is None else int(max_q)
+    # the stride of a dimension of one entry means nothing, and may be anything
+    if total < 2:
+        st = HEAD_DIM
+    sh = HEAD_DIM if hq == 1 else strides[-2]
     if slopes is not None:
         _need(slopes, "slopes", "float32", (hq,), dev)
     if prefix is not None:
@@ -786,7 +792,7 @@ def cache_attend(cache: Cache, table, lens, Q, group_size, cu_q=None, max_q=None
             workspace = _new((nbytes,), (1,), "uint8", dev)
     else:
         nbytes = workspace.numel() * workspace.element_size()
-    spindle_cache_attend(cache.ref, table, width, lens, B, cu_q, max_q, total, Q, dt, group_size, strides[-3], strides[-2],
+    spindle_cache_attend(cache.ref, table, width, lens, B, cu_q, max_q, total, Q, dt, group_size, st, sh,
                          _SCALE if scale is None else scale, softcap, slopes, prefix, q_pos, out, lse, workspace, nbytes)
     return out if lse is None else (out, lse)
 

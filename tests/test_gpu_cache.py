@@ -617,3 +617,30 @@ def test_compact_of_the_largest_numbers(sb, fmt):
     for codes, scale in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
         assert torch.equal(codes[0], codes[1]) and torch.equal(scale[0], scale[1])
         assert torch.isfinite(scale).all() and (codes[0, 0, 5:7, 7:9] != 0).any()
+
+
+# ------------------------------------------------------------------ attention: layouts, scales of any kind, far pages, precision
+
+def test_attend_queries_whose_dimensions_of_one_entry_have_any_stride(sb):
+    """One token a sequence, out of [B, Hq, 1, d] (a decode step's usual order) or out of a longer piece; one head; one sequence."""
+    rng = np.random.default_rng(83)
+    cache, table = filled(sb, rng, [300, 211, 70], 2, 64, "e4m3")
+    t, n = dev(table), dev(np.int32([300, 211, 70]))
+    Q = torch.from_numpy(rng.standard_normal((3, 1, 8, 128)).astype(np.float32)).half().cuda()
+    want, want_lse = sb.cache_attend(cache, t, n, Q, 4, want_lse=True)
+    turned = torch.empty((3, 8, 1, 128), dtype=torch.float16, device="cuda").copy_(Q.transpose(1, 2)).transpose(1, 2)
+    assert turned.stride() == (1024, 128, 128, 1)
+    piece = torch.zeros((3, 5, 8, 128), dtype=torch.float16, device="cuda")
+    piece[:, 4:] = Q
+    for q in (turned, piece[:, 4:], Q.as_strided((3, 1, 8, 128), (1024, 3, 128, 1))):
+        got, lse = sb.cache_attend(cache, t, n, q, 4, want_lse=True)
+        assert torch.equal(got, want) and torch.equal(lse, want_lse)
+    one = sb.cache_attend(cache, t[:1], n[:1], Q[:1].as_strided((1, 1, 8, 128), (7, 5, 128, 1)), 4)
+    assert torch.equal(one, want[:1])
+    ragged = sb.cache_attend(cache, t[:1], n[:1], Q[:1, 0].as_strided((1, 8, 128), (3, 128, 1)), 4, cu_q=dev(np.int32([0, 1])), max_q=1)
+    assert torch.equal(ragged, want[:1, 0])
+    single, rows = filled(sb, rng, [40, 90], 1, 64, "i8")
+    t, n = dev(rows), dev(np.int32([40, 90]))
+    q = torch.from_numpy(rng.standard_normal((2, 3, 1, 128)).astype(np.float32)).half().cuda()
+    want = sb.cache_attend(single, t, n, q, 1)
+    assert torch.equal(sb.cache_attend(single, t, n, q.as_strided((2, 3, 1, 128), (384, 128, 5, 1)), 1), want)
