@@ -718,18 +718,30 @@ def _check_table(cache, table, lens):
     return shape
 
 
+def _row_strides(t):
+    """Strides of all dimensions but the last.  That of a dimension of one entry means nothing and may be anything: it is replaced
+    by one that every call takes."""
+    return [s if n > 1 else HEAD_DIM for s, n in zip(t.stride()[:-1], t.shape)]
+
+
 def cache_append(cache: Cache, table, lens, K, V, cu_new=None, max_new=None, positions=None):
     """Stores new tokens behind the lens [B] that the sequences of table [B, width] hold.  K, V [B, H, m, d] (any order of
     the first three in memory), or, with cu_new [B + 1] int32, [tokens of all, H, d] and max_new, the most tokens of one
-    sequence.  positions [tokens of all] int32.  lens is not changed."""
+    sequence.  positions [tokens of all] int32.  lens is not changed.  The library takes one set of strides for K and V: where theirs
+    differ, those that are not contiguous are copied."""
     B, width = _check_table(cache, table, lens)
     H, dev, shape, strides = cache.n_kv_heads, cache.device, K.shape, K.stride()
-    if V.shape != shape or V.stride() != strides or K.dtype is not V.dtype:
-        raise ValueError("K and V must have the same type, shape and strides")
+    if V.shape != shape or K.dtype is not V.dtype:
+        raise ValueError("K and V must have the same type and shape")
     if K.device != dev or V.device != dev:
         raise ValueError(f"K and V are not on {dev}")
-    if len(shape) != (4 if cu_new is None else 3) or shape[-1] != HEAD_DIM or strides[-1] != 1:
+    if len(shape) != (4 if cu_new is None else 3) or shape[-1] != HEAD_DIM or strides[-1] != 1 or V.stride(-1) != 1:
         raise ValueError(f"K and V are [B, H, m, {HEAD_DIM}], or [tokens, H, {HEAD_DIM}] with cu_new, the last dimension contiguous")
+    if 1 in shape or V.stride() != strides:
+        strides, v_strides = _row_strides(K), _row_strides(V)
+        if strides != v_strides:
+            K, V = K.contiguous(), V.contiguous()
+            strides = _row_strides(K)
     if cu_new is None:
         if shape[0] != B or shape[1] != H:
             raise ValueError(f"K and V must be [{B}, {H}, m, {HEAD_DIM}], got {list(shape)}")

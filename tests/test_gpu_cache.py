@@ -644,3 +644,37 @@ def test_attend_queries_whose_dimensions_of_one_entry_have_any_stride(sb):
     q = torch.from_numpy(rng.standard_normal((2, 3, 1, 128)).astype(np.float32)).half().cuda()
     want = sb.cache_attend(single, t, n, q, 1)
     assert torch.equal(sb.cache_attend(single, t, n, q.as_strided((2, 3, 1, 128), (384, 128, 5, 1)), 1), want)
+
+
+def test_append_of_k_and_v_in_layouts_of_their_own(sb):
+    """K as a rotation leaves it and V as a part of a wider projection; dimensions of one entry, whose strides mean nothing."""
+    rng = np.random.default_rng(89)
+    B, H, m = 3, 4, 21
+    wide = torch.from_numpy(rng.standard_normal((B, m, 3 * H, 128)).astype(np.float32)).half().cuda()
+    K, V = wide[:, :, H:2 * H].transpose(1, 2).contiguous(), wide[:, :, 2 * H:].transpose(1, 2)
+    table, lens = dev(table_of(rng, [2, 2, 2], 2, 8)), dev(np.int32([0, 3, 19]))
+
+    def stored(k, v, at=lens, **kw):
+        cache = sb.new_cache(8, H, 32, "i8")
+        sb.cache_append(cache, table, at, k, v, **kw)
+        return [cache.k, cache.v, cache.k_scale, cache.v_scale]
+
+    def same(a, b):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+    want = stored(K, V.contiguous())
+    same(stored(K, V), want)
+    same(stored(V.contiguous(), K.transpose(1, 2).contiguous().transpose(1, 2)), [want[1], want[0], want[3], want[2]])
+    cu = dev(np.int32([0, m, 2 * m, 3 * m]))
+    rows = [x.transpose(1, 2).reshape(B * m, H, 128) for x in (K, V)]
+    same(stored(rows[0], wide.view(B * m, 3 * H, 128)[:, 2 * H:], cu_new=cu, max_new=m), want)
+    # one token a sequence: one and the same memory has many strides
+    k, v = K[:, :, :1].contiguous(), V[:, :, :1].contiguous()
+    want = stored(k, v)
+    turned = torch.empty((B, 1, H, 128), dtype=torch.float16, device="cuda").copy_(v.transpose(1, 2)).transpose(1, 2)
+    assert turned.stride() != k.stride()
+    same(stored(k, turned), want)
+    same(stored(k.as_strided((B, H, 1, 128), (H * 128, 128, 3, 1)), v), want)
+    # one token in all
+    same(stored(k[:1, :, 0].as_strided((1, H, 128), (5, 128, 1)), v[:1, :, 0], at=lens, cu_new=dev(np.int32([0, 1, 1, 1])), max_new=1),
+         stored(k[:1, :, 0].clone(), v[:1, :, 0].clone(), at=lens, cu_new=dev(np.int32([0, 1, 1, 1])), max_new=1))
