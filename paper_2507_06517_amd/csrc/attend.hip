@@ -494,15 +494,15 @@ extern "C" spindle_status spindle_cache_attend(const spindle_cache *cache, const
   if (spindle_status s = check_cache(cache, &a.c)) return s;
   if (spindle_status s = check_table(table, table_width, len, batch, a.c)) return s;
   if (spindle_status s = check_queries(batch, max_q, total_q, group_size, a.c, cu_q)) return s;
-  if (!Q || !out) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "Q and out are required");
   if (dtype != SPINDLE_F32 && dtype != SPINDLE_F16 && dtype != SPINDLE_BF16) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "unknown dtype %d", dtype);
-  if ((reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(out)) & 15)
-    SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
   if (stride_t < kHeadDim || stride_h < kHeadDim || ((stride_t | stride_h) & 7))
     SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "strides must be >= head_dim and multiples of 8 elements");
   if (!(scale > 0.f) || !(scale < INFINITY)) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "scale must be finite and > 0");
   if (!(softcap >= 0.f) || !(softcap < INFINITY)) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "softcap must be finite and >= 0 (0 = none)");
-  if (max_q == 0 || total_q == 0) return SPINDLE_OK;
+  if (max_q == 0 || total_q == 0) return SPINDLE_OK;                // (tensors without elements have no address)
+  if (!Q || !out) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "Q and out are required");
+  if ((reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(out)) & 15)
+    SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
   const Plan p = plan_attend(a.c, batch, table_width, max_q, total_q, group_size, dtype);
   if (p.bytes && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < p.bytes))
     SPINDLE_FAIL(SPINDLE_ERR_WORKSPACE, "workspace missing, not 256-byte aligned or smaller than %zu bytes", p.bytes);

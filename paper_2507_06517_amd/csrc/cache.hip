@@ -252,16 +252,16 @@ extern "C" spindle_status spindle_cache_append(const spindle_cache *cache, const
   AppendArgs a{};
   if (spindle_status s = check_cache(cache, &a.c)) return s;
   if (spindle_status s = check_table(table, table_width, len, batch, a.c)) return s;
-  if (!K || !V) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "K and V are required");
   if (dtype != SPINDLE_F32 && dtype != SPINDLE_F16 && dtype != SPINDLE_BF16) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "unknown dtype %d", dtype);
   if (max_new < 0 || total_new < 0) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "max_new and total_new must be >= 0");
   if (!cu_new && (int64_t)batch * max_new != total_new)
     SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "without cu_new every sequence gets max_new tokens: total_new must be batch * max_new");
   if (stride_b < 0 || stride_h < kHeadDim || stride_t < kHeadDim) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "strides must be >= 0, those of heads and tokens >= head_dim");
   if ((stride_b | stride_h | stride_t) & 7) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "strides must be multiples of 8 elements");
+  if (max_new == 0 || total_new == 0) return SPINDLE_OK;            // (tensors without elements have no address)
+  if (!K || !V) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "K and V are required");
   if ((reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) & 15)
     SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
-  if (max_new == 0 || total_new == 0) return SPINDLE_OK;
   const int elt = dtype_bytes(dtype);
   a.table = table, a.len = len, a.cu = cu_new, a.positions = positions;
   a.K = static_cast<const char *>(K), a.V = static_cast<const char *>(V);
@@ -308,8 +308,9 @@ extern "C" spindle_status spindle_cache_compact(const spindle_cache *cache, cons
 extern "C" spindle_status spindle_cache_copy(const spindle_cache *cache, const int32_t *pairs, int32_t n_pairs, void *stream) {
   CacheView c;
   if (spindle_status s = check_cache(cache, &c)) return s;
-  if (!pairs || n_pairs < 0) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "pairs is required and n_pairs must be >= 0");
+  if (n_pairs < 0) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "n_pairs must be >= 0");
   if (n_pairs == 0) return SPINDLE_OK;
+  if (!pairs) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "pairs is required");
   if ((int64_t)n_pairs * c.H >= kMostBlocks) SPINDLE_FAIL(SPINDLE_ERR_UNSUPPORTED, "too many pages in one call: split the pairs");
   hipStream_t st = static_cast<hipStream_t>(stream);
   {

@@ -200,3 +200,13 @@ def test_grids_that_a_launch_cannot_hold_are_refused(sb):
     assert compact(sb, wide, batch=32767) == 2
     assert sb.lib().spindle_cache_copy(wide, FAKE, 1 << 20, None) == 2
     assert append(sb, desc(sb, n_pages=1 << 29, heads=2)) == 2
+
+
+def test_calls_without_tokens_take_no_pointers(sb):
+    """Tensors without elements have no address."""
+    assert append(sb, max_new=0, K=None, V=None) == 0 and append(sb, total=0, K=None, V=None) == 0
+    assert attend(sb, max_q=0, Q=None, out=None) == 0 and attend(sb, total=0, Q=None, out=None) == 0
+    assert attend(sb, cu=None, batch=2, max_q=0, total=0, Q=None, out=None, ws=None, wsb=0) == 0
+    assert sb.lib().spindle_cache_copy(desc(sb), None, 0, None) == 0
+    assert append(sb, max_new=0, dtype=3) == 1 and attend(sb, max_q=0, scale=0.0) == 1     # everything else is looked at
+    assert sb.lib().spindle_cache_copy(desc(sb), None, 1, None) == 1

@@ -678,3 +678,17 @@ def test_append_of_k_and_v_in_layouts_of_their_own(sb):
     # one token in all
     same(stored(k[:1, :, 0].as_strided((1, H, 128), (5, 128, 1)), v[:1, :, 0], at=lens, cu_new=dev(np.int32([0, 1, 1, 1])), max_new=1),
          stored(k[:1, :, 0].clone(), v[:1, :, 0].clone(), at=lens, cu_new=dev(np.int32([0, 1, 1, 1])), max_new=1))
+
+
+def test_calls_without_tokens(sb):
+    rng = np.random.default_rng(131)
+    cache, table = filled(sb, rng, [40, 90], 2, 64, "i8")
+    t, n, before = dev(table), dev(np.int32([40, 90])), pools_of(cache)
+    q, kv = torch.empty((2, 0, 8, 128), dtype=torch.float16, device="cuda"), torch.empty((2, 2, 0, 128), device="cuda")
+    assert sb.cache_attend(cache, t, n, q, 4).shape == (2, 0, 8, 128)
+    out, lse = sb.cache_attend(cache, t, n, q.view(0, 8, 128), 4, cu_q=dev(np.int32([0, 0, 0])), want_lse=True)
+    assert out.shape == (0, 8, 128) and lse.shape == (0, 8)
+    sb.cache_append(cache, t, n, kv, kv)
+    sb.cache_append(cache, t, n, kv.view(0, 2, 128), kv.view(0, 2, 128), cu_new=dev(np.int32([0, 0, 0])))
+    sb.cache_copy(cache, torch.empty((0, 2), dtype=torch.int32, device="cuda"))
+    same_pools(cache, before)
