@@ -803,6 +803,8 @@ def cache_attend(cache: Cache, table, lens, Q, group_size, cu_q=None, max_q=None
         if nbytes:
             workspace = _new((nbytes,), (1,), "uint8", dev)
     else:
+        if workspace.device != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous tensor on {dev}")
         nbytes = workspace.numel() * workspace.element_size()
     spindle_cache_attend(cache.ref, table, width, lens, B, cu_q, max_q, total, Q, dt, group_size, st, sh,
                          _SCALE if scale is None else scale, softcap, slopes, prefix, q_pos, out, lse, workspace, nbytes)

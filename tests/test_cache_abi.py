@@ -210,3 +210,17 @@ def test_calls_without_tokens_take_no_pointers(sb):
     assert sb.lib().spindle_cache_copy(desc(sb), None, 0, None) == 0
     assert append(sb, max_new=0, dtype=3) == 1 and attend(sb, max_q=0, scale=0.0) == 1     # everything else is looked at
     assert sb.lib().spindle_cache_copy(desc(sb), None, 1, None) == 1
+
+
+def test_given_workspaces_are_looked_at(sb):
+    """The library gets its address: it has to be on the cache's device and in one piece."""
+    import torch
+    cache = sb.new_cache(64, 1, 64, "i8", device="cpu")
+    table, lens = torch.zeros((1, 60), dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    q = torch.zeros((1, 1, 4, 128), dtype=torch.float16)
+    n = sb.spindle_attend_workspace_bytes(cache.ref, 1, 60, 1, 1, 4, sb.F16)
+    assert n > 0
+    with pytest.raises(ValueError, match="workspace"):
+        sb.cache_attend(cache, table, lens, q, 4, workspace=torch.empty(n, dtype=torch.uint8, device="meta"))
+    with pytest.raises(ValueError, match="workspace"):
+        sb.cache_attend(cache, table, lens, q, 4, workspace=torch.empty(2 * n, dtype=torch.uint8)[::2])
