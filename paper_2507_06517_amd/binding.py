@@ -138,6 +138,16 @@ def _stream():
     return _raw_stream(_current_device())
 
 
+def _stream_on(device):
+    """_stream() for tensors of this device: kernels run on the current one and get plain addresses."""
+    if device.type != "cuda":
+        raise ValueError(f"the tensors are on {device}, not on a GPU")
+    stream = _stream()
+    if device.index != _current_device():
+        raise ValueError(f"the tensors are on {device}, the current device is {_current_device()}")
+    return stream
+
+
 def torch_dtype(dtype: str):
     import torch
     return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[dtype]
@@ -755,7 +765,8 @@ def cache_append(cache: Cache, table, lens, K, V, cu_new=None, max_new=None, pos
         max_new = total if max_new is None else int(max_new)
     if positions is not None:
         _ints(positions, "positions", (total,), dev)
-    spindle_cache_append(cache.ref, table, width, lens, B, cu_new, max_new, total, K, V, _dtype_of(K), sb, sh, st, positions)
+    spindle_cache_append(cache.ref, table, width, lens, B, cu_new, max_new, total, K, V, _dtype_of(K), sb, sh, st, positions,
+                         _stream_on(dev))
 
 
 def cache_attend(cache: Cache, table, lens, Q, group_size, cu_q=None, max_q=None, scale=None, softcap=0.0, slopes=None, prefix=None,
@@ -807,7 +818,8 @@ def cache_attend(cache: Cache, table, lens, Q, group_size, cu_q=None, max_q=None
             raise ValueError(f"workspace must be a contiguous tensor on {dev}")
         nbytes = workspace.numel() * workspace.element_size()
     spindle_cache_attend(cache.ref, table, width, lens, B, cu_q, max_q, total, Q, dt, group_size, st, sh,
-                         _SCALE if scale is None else scale, softcap, slopes, prefix, q_pos, out, lse, workspace, nbytes)
+                         _SCALE if scale is None else scale, softcap, slopes, prefix, q_pos, out, lse, workspace, nbytes,
+                         _stream_on(dev))
     return out if lse is None else (out, lse)
 
 
@@ -819,14 +831,14 @@ def cache_compact(cache: Cache, table, lens, kept, n_kept, table_out):
     _ints(kept, "kept", (B, cache.n_kv_heads, stride), dev)
     _ints(n_kept, "n_kept", (B,), dev)
     _ints(table_out, "table_out", (B, width_out), dev)
-    spindle_cache_compact(cache.ref, table, width, lens, B, kept, stride, n_kept, table_out, width_out)
+    spindle_cache_compact(cache.ref, table, width, lens, B, kept, stride, n_kept, table_out, width_out, _stream_on(dev))
 
 
 def cache_copy(cache: Cache, copies):
     """Copies pages, copies [n, 2] int32 (from, to); -1 copies nothing."""
     n = copies.shape[0]
     _ints(copies, "copies", (n, 2), cache.device)
-    spindle_cache_copy(cache.ref, copies, n)
+    spindle_cache_copy(cache.ref, copies, n, _stream_on(cache.device))
 
 
 def _check_pages(refs, table, lens):
@@ -845,7 +857,7 @@ def pages_share(refs, table, lens, parent, page_tokens):
     rows = parent.shape[0]
     _ints(parent, "parent", (rows,), dev)
     out, n = _new((rows, width), (width, 1), "int32", dev), _new((rows,), (1,), "int32", dev)
-    spindle_pages_share(refs, n_pages, table, lens, rows_in, width, page_tokens, parent, rows, out, n)
+    spindle_pages_share(refs, n_pages, table, lens, rows_in, width, page_tokens, parent, rows, out, n, _stream_on(dev))
     return out, n
 
 
@@ -857,11 +869,11 @@ def pages_reserve(refs, table, lens, grow, page_tokens):
     n, copies, status = _new((rows,), (1,), "int32", dev), _new((rows, 2), (2, 1), "int32", dev), _new((2,), (1,), "int32", dev)
     nws = (n_pages + 63) // 64 * 64                # spindle_pages_workspace_bytes in ints
     ws = _new((nws,), (1,), "int32", dev)
-    spindle_pages_reserve(refs, n_pages, table, lens, grow, rows, width, page_tokens, n, copies, status, ws, 4 * nws)
+    spindle_pages_reserve(refs, n_pages, table, lens, grow, rows, width, page_tokens, n, copies, status, ws, 4 * nws, _stream_on(dev))
     return n, copies, status
 
 
 def pages_release(refs, table, lens, page_tokens):
     """The rows' pages are held once less."""
-    _, rows, width, n_pages = _check_pages(refs, table, lens)
-    spindle_pages_release(refs, n_pages, table, lens, rows, width, page_tokens)
+    dev, rows, width, n_pages = _check_pages(refs, table, lens)
+    spindle_pages_release(refs, n_pages, table, lens, rows, width, page_tokens, _stream_on(dev))

@@ -224,3 +224,22 @@ def test_given_workspaces_are_looked_at(sb):
         sb.cache_attend(cache, table, lens, q, 4, workspace=torch.empty(n, dtype=torch.uint8, device="meta"))
     with pytest.raises(ValueError, match="workspace"):
         sb.cache_attend(cache, table, lens, q, 4, workspace=torch.empty(2 * n, dtype=torch.uint8)[::2])
+
+
+def test_tensors_that_are_not_on_the_current_gpu_are_refused(sb, monkeypatch):
+    """Calls that fit in every other way: kernels must not get addresses of host memory, nor run beside the tensors' device."""
+    import torch
+    cache = sb.new_cache(4, 2, 64, "i8", device="cpu")
+    table, lens = torch.zeros((1, 2), dtype=torch.int32), torch.ones(1, dtype=torch.int32)
+    kv, q, refs = torch.zeros((1, 2, 3, 128)), torch.zeros((1, 1, 8, 128)), torch.zeros(4, dtype=torch.int32)
+    for call in (lambda: sb.cache_append(cache, table, lens, kv, kv), lambda: sb.cache_attend(cache, table, lens, q, 4),
+                 lambda: sb.cache_compact(cache, table, lens, torch.zeros((1, 2, 5), dtype=torch.int32), lens, table),
+                 lambda: sb.cache_copy(cache, torch.zeros((1, 2), dtype=torch.int32)), lambda: sb.pages_share(refs, table, lens, lens, 64),
+                 lambda: sb.pages_reserve(refs, table, lens, lens, 64), lambda: sb.pages_release(refs, table, lens, 64)):
+        with pytest.raises(ValueError, match="not on a GPU"):
+            call()
+    monkeypatch.setattr(sb, "_raw_stream", lambda device: 7 + device)
+    monkeypatch.setattr(sb, "_current_device", lambda: 0)
+    assert sb._stream_on(torch.device("cuda", 0)) == 7
+    with pytest.raises(ValueError, match="current device"):
+        sb._stream_on(torch.device("cuda", 1))
