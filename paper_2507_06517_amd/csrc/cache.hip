@@ -291,7 +291,7 @@ extern "C" spindle_status spindle_cache_compact(const spindle_cache *cache, cons
   if (!kept_idx || kept_stride < 1) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "kept_idx is required and kept_stride must be >= 1");
   a.table = table, a.len = len, a.kept = kept_idx, a.n_kept = n_kept, a.table_out = table_out;
   a.width = table_width, a.width_out = out_width, a.kept_stride = kept_stride;
-  a.tiles = (kept_stride + a.c.P - 1) / a.c.P;
+  a.tiles = (int)(((int64_t)kept_stride + a.c.P - 1) / a.c.P);
   if (a.tiles > out_width) a.tiles = out_width;
   const int64_t blocks = (int64_t)batch * a.tiles * a.c.H * 2;
   if (blocks >= kMostBlocks) SPINDLE_FAIL(SPINDLE_ERR_UNSUPPORTED, "too many pages in one call: split the batch");

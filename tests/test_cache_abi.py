@@ -243,3 +243,10 @@ def test_tensors_that_are_not_on_the_current_gpu_are_refused(sb, monkeypatch):
     assert sb._stream_on(torch.device("cuda", 0)) == 7
     with pytest.raises(ValueError, match="current device"):
         sb._stream_on(torch.device("cuda", 1))
+
+
+def test_sizes_next_to_the_largest_integers(sb):
+    """No sum of the sizes wraps around on the way to a grid: each of these asks for more than a launch holds."""
+    wide = desc(sb, heads=1024)
+    assert compact(sb, wide, batch=32767, stride=2 ** 31 - 1, out_width=4) == 2
+    assert append(sb, wide, batch=32767, max_new=2 ** 31 - 1, total=2 ** 31 - 1, width=4) == 2
