@@ -163,6 +163,7 @@ spindle_status check_pages(const void *refs, int32_t n_pages, const void *table,
                            int32_t page_tokens, int *shift) {
   if (!refs || !table || !len) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "refs, table and len are required");
   if (n_pages < 1 || width < 1 || rows < 1) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "n_pages, the table's width and its rows must be >= 1");
+  if (n_pages >= (1 << 30)) SPINDLE_FAIL(SPINDLE_ERR_UNSUPPORTED, "n_pages must be below 2^30");
   if (page_tokens != 32 && page_tokens != 64 && page_tokens != 128 && page_tokens != 256)
     SPINDLE_FAIL(SPINDLE_ERR_UNSUPPORTED, "page_tokens must be 32, 64, 128 or 256, got %d", page_tokens);
   if ((int64_t)width * page_tokens > (1 << 30)) SPINDLE_FAIL(SPINDLE_ERR_UNSUPPORTED, "a table's row may hold at most 2^30 tokens");
@@ -211,6 +212,7 @@ extern "C" spindle_status spindle_pages_release(int32_t *refs, int32_t n_pages, 
 extern "C" spindle_status spindle_pages_workspace_bytes(int32_t n_pages, size_t *bytes) {
   if (!bytes) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "bytes is NULL");
   if (n_pages < 1) SPINDLE_FAIL(SPINDLE_ERR_INVALID_ARG, "n_pages must be >= 1");
+  if (n_pages >= (1 << 30)) SPINDLE_FAIL(SPINDLE_ERR_UNSUPPORTED, "n_pages must be below 2^30");
   *bytes = align_up((size_t)n_pages * 4, 256);
   return SPINDLE_OK;
 }

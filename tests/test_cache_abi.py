@@ -250,3 +250,13 @@ def test_sizes_next_to_the_largest_integers(sb):
     wide = desc(sb, heads=1024)
     assert compact(sb, wide, batch=32767, stride=2 ** 31 - 1, out_width=4) == 2
     assert append(sb, wide, batch=32767, max_new=2 ** 31 - 1, total=2 ** 31 - 1, width=4) == 2
+
+
+def test_counts_of_more_pages_than_a_pool_has_are_refused(sb):
+    """The bookkeeping counts pages in steps of 16384, which must not pass the largest integer; a pool ends at 2^30."""
+    L, n = sb.lib(), C.c_size_t(0)
+    for n_pages in (2 ** 30, 2 ** 31 - 1):
+        assert L.spindle_pages_share(FAKE, n_pages, FAKE, FAKE, 2, 4, 64, FAKE, 2, 0x2000, 0x2000, None) == 2
+        assert L.spindle_pages_reserve(FAKE, n_pages, FAKE, FAKE, FAKE, 2, 4, 64, 0x2000, FAKE, FAKE, FAKE, 1 << 40, None) == 2
+        assert L.spindle_pages_release(FAKE, n_pages, FAKE, FAKE, 2, 4, 64, None) == 2
+        assert L.spindle_pages_workspace_bytes(n_pages, C.byref(n)) == 2
