@@ -92,7 +92,7 @@ __global__ __launch_bounds__(kWaves * 64, DT == SPINDLE_F32 ? 3 : 4) void attend
   const int t0 = cu0, m = min(max(cu1 - cu0, 0), a.max_q);
   const int rows = m * a.group, row_begin = row_tile * (kRows);
   const int first_q = len_b - m;                 // slot of the first new token
-  if (row_begin >= rows || t0 < 0 || t0 + m > a.total_q || (begin >= len && split > 0)) return;
+  if (row_begin >= rows || t0 < 0 || t0 > a.total_q - m || (begin >= len && split > 0)) return;
   // the rows are in the order of their tokens: the first sees least, the last most
   const int last_row = min(row_begin + kRows, rows) - 1;
   const int least = max(min(first_q + row_begin / a.group + 1, len), prefix);
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(32 * kJoinGroups) void attend_join(AttendArgs a) {
   const int b = blockIdx.x / a.max_q, i = blockIdx.x % a.max_q, hq = blockIdx.y;
   const int t0 = a.cu ? a.cu[b] : b * a.max_q;
   const int m = a.cu ? min(max(a.cu[b + 1] - t0, 0), a.max_q) : a.max_q;
-  if (i >= m || t0 < 0 || t0 + m > a.total_q) return;
+  if (i >= m || t0 < 0 || t0 > a.total_q - m) return;
   const size_t at = (size_t)(t0 + i) * a.heads_q + hq;
   const int d = threadIdx.x & 31, group = threadIdx.x >> 5;
   const float2 *ml = a.part_ml + at * a.splits;
@@ -313,7 +313,7 @@ __global__ __launch_bounds__(32 * kJoinGroups) void attend_join_few(AttendArgs a
   if (b >= a.batch) return;
   const int t0 = a.cu ? a.cu[b] : b * a.max_q;
   const int m = a.cu ? min(max(a.cu[b + 1] - t0, 0), a.max_q) : a.max_q;
-  if (i >= m || t0 < 0 || t0 + m > a.total_q) return;
+  if (i >= m || t0 < 0 || t0 > a.total_q - m) return;
   const size_t at = (size_t)(t0 + i) * a.heads_q + hq;
   const float2 *ml = a.part_ml + at * a.splits;
   const f4 *po = reinterpret_cast<const f4 *>(a.part_o + at * a.splits * kHeadDim) + d;

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
   const int m = a.cu ? min(max(a.cu[b + 1] - t0, 0), a.max_q) : a.max_q;
   const int rows = m * a.group, row_begin = row_tile * kManyRows;
   const int begin = split * kStep, stride = a.splits * kStep, first_q = a.len[b] - m;
-  if (row_begin >= rows || t0 < 0 || t0 + m > a.total_q || (begin >= len && split > 0)) return;
+  if (row_begin >= rows || t0 < 0 || t0 > a.total_q - m || (begin >= len && split > 0)) return;
   const int prefix = a.prefix ? min(max(a.prefix[b], 0), len) : 0;
   auto limit_of = [&](int row) { return max(min(first_q + row / a.group + 1, len), prefix); };
   const int end = limit_of(min(row_begin + kManyRows, rows) - 1);

@@ -692,3 +692,22 @@ def test_calls_without_tokens(sb):
     sb.cache_append(cache, t, n, kv.view(0, 2, 128), kv.view(0, 2, 128), cu_new=dev(np.int32([0, 0, 0])))
     sb.cache_copy(cache, torch.empty((0, 2), dtype=torch.int32, device="cuda"))
     same_pools(cache, before)
+
+
+@pytest.mark.parametrize("dtype,m", [("f16", 3), ("bf16", 40), ("f32", 3)])
+def test_attend_leaves_sequences_whose_queries_lie_outside(sb, dtype, m):
+    """Starts that are negative, behind the queries, or so large that the sum with a count wraps around: nothing is read or written
+    for them (sequences in chunks and whole ones)."""
+    rng = np.random.default_rng(137)
+    lens, top = [1200, 70, 1200], 2 ** 31 - 1
+    for width in (64, 20):
+        cache, table = filled(sb, rng, lens, 1, 64, "e4m3", width=width)
+        Q = torch.from_numpy(rng.standard_normal((m, 4, 128)).astype(np.float32)).to(DT[dtype]).cuda()
+        want = sb.cache_attend(cache, dev(table[1:2]), dev(np.int32(lens[1:2])), Q, 4, cu_q=dev(np.int32([0, m])), max_q=m)
+        for cu in ([-5, 0, m, m + 2], [m + 1, 0, m, top], [-2 ** 31, 0, m, m + 1], [top, -2 ** 31 + 5, top]):
+            out, lse, B = torch.full_like(Q, 9.0), torch.full((m, 4), 9.0, device="cuda"), len(cu) - 1
+            sb.cache_attend(cache, dev(table[:B]), dev(np.int32(lens[:B])), Q, 4, cu_q=dev(np.int32(cu)), max_q=m, out=out, lse=lse)
+            if B == 2:
+                assert (out == 9).all() and (lse == 9).all()
+            else:                                                    # (another number of chunks: two results within their bounds)
+                assert (out - want).abs().max().item() <= max(2 * float(torch.finfo(DT[dtype]).eps), 2.0 ** -16) * want.abs().max().item(), cu
