@@ -443,7 +443,9 @@ typedef enum {
 
 /*
  * The pools of one layer.  A page holds page_tokens tokens of every KV head; token t of a sequence is in slot
- * t % page_tokens of page table[row][t / page_tokens].  A code stands for code * scale of its page and head.
+ * t % page_tokens of page table[row][t / page_tokens].  A code stands for code * scale of its page and head, whatever positive scale
+ * a pool was filled with; what the calls here write for E4M3 are powers of two.  (Appending to a page with another E4M3 scale
+ * divides with a rounding, and a value next to the middle between two codes may get either.)
  * pos, if not NULL, is the position of each slot's token (kept tokens of an eviction have gaps, other ones for each head);
  * a slot whose position is negative is empty: attention does not see it.
  * Entries of a table or of kept_idx that are out of range are treated as absent: nothing is read or written through them.

@@ -69,8 +69,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
     load_query<DT, 8>(q, a.Q + (size_t)(t0 + i) * a.qst + (size_t)hq * a.qsh, on, [g](int k) { return 16 * k + 8 * g; });
   }
   const float factor = kMode == kPlain ? a.scale * kLog2e : a.scale;
-  // E4M3's scales are powers of two and go into V's bf16 operands for nothing.  Other operands are the codes, counting
-  // `ref` (the largest scale so far) each, and the weights are multiplied.
+  // E4M3's scales are powers of two and go into V's bf16 operands for nothing (of a scale that is none, from a pool that was
+  // filled elsewhere, what is left over goes into the weights).  Other operands are the codes, counting `ref` (the
+  // largest scale so far) each, and the weights are multiplied.
   constexpr bool kTrueV = FMT == SPINDLE_E4M3 && DT == SPINDLE_BF16;
   float ref = kTrueV ? 1.f : kTinyScale;
 
@@ -144,7 +145,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
       char *const to = v_to + buffer * kBuffer + h * (8 * kFrag);
 #pragma unroll
       for (int e = 0; e < 4; e += 2) {           // (8 bytes of each of two dimensions at a time)
-        const u4 w = __builtin_bit_cast(u4, N::template codes<FMT>(col[e], col[e + 1], kTrueV && next[h].there ? next[h].vs : 1.f));
+        const u4 w = __builtin_bit_cast(u4, N::template codes<FMT>(col[e], col[e + 1], kTrueV && next[h].there ? power_of(next[h].vs) : 1.f));
         *reinterpret_cast<u2 *>(to + ((v_lane0 + e) ^ v_turn) * 16) = u2{w[0], w[1]};
         *reinterpret_cast<u2 *>(to + ((v_lane0 + e + 1) ^ v_turn) * 16) = u2{w[2], w[3]};
       }
@@ -209,6 +210,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
       // (2^-60) is multiplied in at the end, where the sum cannot lose it
       float log_v[2] = {0.f, 0.f}, per_v[2] = {1.f, 1.f}, rest_v[2] = {1.f, 1.f}, vback = 1.f;
       bool scaled = false, tiny_v = false;
+      const bool odd_v = kTrueV && ((__float_as_uint(here[0].vs) | __float_as_uint(here[1].vs)) & 0x7FFFFFu) != 0;
       if (!kTrueV) {
         const float v[2] = {there[0] ? here[0].vs : 0.f, there[1] ? here[1].vs : 0.f};
         const float was = ref;
@@ -245,12 +247,17 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
           }
         }
       }
-      if (t + kStep > least || !there[0] || !there[1]) {
+      if (t + kStep > least || !there[0] || !there[1] || odd_v) {   // (one branch for all that is rare)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             if (t + 32 * h + 8 * (e >> 2) + 4 * g + (e & 3) >= st.limit || !there[h]) s[h][e] = -INFINITY;
+          if (kTrueV && there[h] && here[h].vs > 0.f) {
+            log_v[h] = __builtin_amdgcn_logf(here[h].vs * (1.f / power_of(here[h].vs)));   // 0 of a power of two
+            per_v[h] = __builtin_amdgcn_exp2f(-log_v[h]);
+          }
+        }
       }
       float top[2] = {s[0][0], s[1][0]};
 #pragma unroll
@@ -268,7 +275,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
           w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + j], slope[u >> 1], from));
           sum += w[j];
         }
-        st.l += kTrueV ? sum : sum * per_v[u >> 1];
+        st.l = __builtin_fmaf(sum, per_v[u >> 1], st.l);
         if (!kTrueV && tiny_v) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) w[j] *= rest_v[u >> 1];

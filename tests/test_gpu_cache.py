@@ -711,3 +711,19 @@ def test_attend_leaves_sequences_whose_queries_lie_outside(sb, dtype, m):
                 assert (out == 9).all() and (lse == 9).all()
             else:                                                    # (another number of chunks: two results within their bounds)
                 assert (out - want).abs().max().item() <= max(2 * float(torch.finfo(DT[dtype]).eps), 2.0 ** -16) * want.abs().max().item(), cu
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_attend_scales_that_are_no_powers_of_two(sb, dtype):
+    """A code stands for code times scale, whatever the scale of a pool that somebody else filled; few rows and many."""
+    rng = np.random.default_rng(97)
+    lens = [130, 300]
+    cache, table = filled(sb, rng, lens, 2, 64, "e4m3")
+    for scale in (cache.k_scale, cache.v_scale):
+        scale.mul_(dev(rng.uniform(1, 2, scale.shape).astype(np.float32)))
+    check_attend(sb, rng, cache, table, lens, [1, 2], 4, dtype)
+    check_attend(sb, rng, cache, table, lens, [40, 25], 4, dtype)
+    cache.v_scale.fill_(2.0 ** -126 * 0.75)                           # below the smallest normal number
+    cache.k_scale.fill_(1.5)
+    got, _ = check_attend(sb, rng, cache, table, lens, [40, 25], 4, dtype)
+    assert torch.isfinite(got.float()).all()
