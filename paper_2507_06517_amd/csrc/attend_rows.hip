@@ -248,16 +248,19 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
         }
       }
       if (t + kStep > least || !there[0] || !there[1] || odd_v) {   // (one branch for all that is rare)
+        if (odd_v) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (t + 32 * h + 8 * (e >> 2) + 4 * g + (e & 3) >= st.limit || !there[h]) s[h][e] = -INFINITY;
-          if (kTrueV && there[h] && here[h].vs > 0.f) {
+          for (int h = 0; h < 2; ++h) {
+            if (!there[h] || !(here[h].vs > 0.f)) continue;
             log_v[h] = __builtin_amdgcn_logf(here[h].vs * (1.f / power_of(here[h].vs)));   // 0 of a power of two
             per_v[h] = __builtin_amdgcn_exp2f(-log_v[h]);
           }
         }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (t + 32 * h + 8 * (e >> 2) + 4 * g + (e & 3) >= st.limit || !there[h]) s[h][e] = -INFINITY;
       }
       float top[2] = {s[0][0], s[1][0]};
 #pragma unroll
