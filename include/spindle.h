@@ -504,8 +504,8 @@ spindle_status spindle_attend_workspace_bytes(const spindle_cache *cache, int32_
  *   prefix       optional [batch] int32
  *   q_pos        optional [total_q] int32 positions of the queries; NULL = their places in the sequence
  *   out          [total_q, n_kv_heads * group_size, 128] contiguous, `dtype`;  lse optional [total_q, n_kv_heads * group_size] f32
- * Products are of f16 operands (f16 queries) or bf16 operands, with f32 sums: codes and 16-bit queries are exact in them, f32 queries
- * are three bf16 each; softmax weights are one f16 (11 bits), two bf16 (bf16 queries) or three (f32).  Statistics are f32.
+ * Products are of 16-bit operands with f32 sums: codes and 16-bit queries are exact in them, f32 queries are three bf16 each; softmax
+ * weights are two bf16 (16 bits, for 16-bit queries) or three (f32).  Statistics are f32.
  */
 spindle_status spindle_cache_attend(const spindle_cache *cache, const int32_t *table, int32_t table_width,
                                     const int32_t *len, int32_t batch, const int32_t *cu_q, int32_t max_q,

@@ -8,18 +8,13 @@ namespace spindle {
 constexpr int kRows = 16;                        // query rows of a matrix instruction
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// What the matrix instructions are fed.  Codes are exact in f16 and in bf16.  f16 queries and their weights are f16 (weights
-// as 2^13 p: those below 2^-38 of a row's largest fall off, far under the output's own step).  bf16 and f32 have bf16's
-// range, where no weight falls off: a bf16 query is one operand, its weights two (16 bits of mantissa), f32 queries and
-// weights are three (24 bits).
-//
-// kSlack: a row's weights are counted from a logit that its largest one may exceed by so much (log2) before what was
-// gathered is scaled down; f16 weights then stay below 2^16.
-template <int DT>
-struct Num {
+// What the matrix instructions are fed.  Codes are exact in f16 and in bf16, and so are 16-bit queries in their own type; f32
+// queries are three bf16 (24 bits).  The softmax's weights are bf16 whatever the queries are, two for 16-bit queries (16 bits) and
+// three for f32 (24): bf16 has float's range, where no weight falls off, and none loses bits because its page's scale is far
+// below another's.  One f16 would hold 11 bits over a factor of 2^38, V's scale included; it is 11 % faster for f16 prompts with
+// capped scores (59 and 66 us for five of up to 1500 tokens) and 1 % for a token over a long context.
+struct Bf16Operand {
   typedef b8 frag;
-  static constexpr int kQ = DT == SPINDLE_F32 ? 3 : 1, kP = DT == SPINDLE_F32 ? 3 : 2;
-  static constexpr float kLift = 0.f, kSlack = 8.f;
   static __device__ __forceinline__ f4 mma(frag x, frag y, f4 z) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, z, 0, 0, 0); }
   static __device__ __forceinline__ f16v mma32(frag x, frag y, f16v z) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, z, 0, 0, 0); }
   // x as the sum of n operands: leading 16 bits, and what is left (exact but for the last one)
@@ -49,29 +44,44 @@ struct Num {
     return __builtin_bit_cast(frag, w);
   }
 };
-template <>
-struct Num<SPINDLE_F16> {
+
+struct F16Operand {
   typedef h8 frag;
-  static constexpr int kQ = 1, kP = 1;
-  static constexpr float kLift = 13.f, kSlack = 2.f;
   static __device__ __forceinline__ f4 mma(frag x, frag y, f4 z) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, z, 0, 0, 0); }
   static __device__ __forceinline__ f16v mma32(frag x, frag y, f16v z) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, z, 0, 0, 0); }
   template <int n>
   static __device__ __forceinline__ void split(const float *x, frag *out) {
+    static_assert(n == 1, "f16 queries are one operand");
 #pragma unroll
     for (int j = 0; j < 8; ++j) out[0][j] = (_Float16)x[j];
   }
   template <int FMT>
-  static __device__ __forceinline__ frag codes(uint32_t lo, uint32_t hi, float scale = 1.f) {
+  static __device__ __forceinline__ frag codes(uint32_t lo, uint32_t hi) {
     union {
       h8 v;
       h2 p[4];
     } r;
-    Code<FMT>::to_half(lo, scale, &r.p[0], &r.p[1]);
-    Code<FMT>::to_half(hi, scale, &r.p[2], &r.p[3]);
+    Code<FMT>::to_half(lo, &r.p[0], &r.p[1]);
+    Code<FMT>::to_half(hi, &r.p[2], &r.p[3]);
     return r.v;
   }
 };
+
+template <int DT>
+struct Num {
+  typedef Bf16Operand Q;                         // of queries and K
+  static constexpr int kQ = DT == SPINDLE_F32 ? 3 : 1, kP = DT == SPINDLE_F32 ? 3 : 2;
+};
+template <>
+struct Num<SPINDLE_F16> {
+  typedef F16Operand Q;
+  static constexpr int kQ = 1, kP = 2;
+};
+typedef Bf16Operand Weights;                     // of the weights and V
+
+// A row's weights are counted from a logit that its largest one may exceed by so much (log2) before what was gathered is
+// scaled down.
+constexpr float kSlack = 8.f;
 
 struct AttendArgs {
   CacheView c;
@@ -138,9 +148,8 @@ __device__ __forceinline__ float over_groups_sum(float v) {
 }
 
 // log sum exp of a row from its reference logit (log2) and sum; a row that sees nothing has -inf, NaN stays.
-template <int DT>
 __device__ __forceinline__ float lse_of(float top, float sum) {
-  return sum > 0.f ? (top + __builtin_amdgcn_logf(sum) - Num<DT>::kLift) / kLog2e : sum == sum ? -INFINITY : sum;
+  return sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) / kLog2e : sum == sum ? -INFINITY : sum;
 }
 
 // What a row of the tile is, and what it has gathered so far.
@@ -153,7 +162,7 @@ struct RowState {
 
 // A lane's part of a query row as the operands of kSteps steps, those of step s from dimension offset_of(s) on.
 template <int DT, int kSteps, typename Where>
-__device__ __forceinline__ void load_query(typename Num<DT>::frag (*q)[Num<DT>::kQ], const char *src, bool on, Where offset_of) {
+__device__ __forceinline__ void load_query(typename Num<DT>::Q::frag (*q)[Num<DT>::kQ], const char *src, bool on, Where offset_of) {
   typedef typename Elem<DT>::type T;
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
@@ -162,7 +171,7 @@ __device__ __forceinline__ void load_query(typename Num<DT>::frag (*q)[Num<DT>::
     if (on) __builtin_memcpy(e, __builtin_assume_aligned(src + offset_of(s) * sizeof(T), 16), sizeof(e));
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = on ? Elem<DT>::to_float(e[j]) : 0.f;
-    Num<DT>::template split<Num<DT>::kQ>(v, q[s]);
+    Num<DT>::Q::template split<Num<DT>::kQ>(v, q[s]);
   }
 }
 
@@ -205,9 +214,8 @@ __device__ __forceinline__ float logit_offset(const AttendArgs &a) {
 
 // Takes the largest logit of a row's step: what was gathered is scaled down (by what is returned) if it has grown by more than
 // the slack.
-template <int DT>
 __device__ __forceinline__ float gather(RowState &st, float top, bool *scaled) {
-  const bool grown = top > st.m + Num<DT>::kSlack;                  // -inf at first: then any logit is more
+  const bool grown = top > st.m + kSlack;                  // -inf at first: then any logit is more
   *scaled = __any(grown);
   if (!*scaled) return 1.f;
   const float back = grown ? __builtin_amdgcn_exp2f(st.m - top) : 1.f;   // 2^-inf is 0

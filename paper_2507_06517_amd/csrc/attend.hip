@@ -70,7 +70,7 @@ template <int DT, int FMT, int kMode, int kWaves>
 __global__ __launch_bounds__(kWaves * 64, DT == SPINDLE_F32 ? 3 : 4) void attend(AttendArgs a) {
   typedef typename Elem<DT>::type T;
   typedef Num<DT> N;
-  typedef typename N::frag frag;
+  typedef typename N::Q Q;
   const CacheView &c = a.c;
   const int lane = lane_id(), x = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(kWaves * 64, DT == SPINDLE_F32 ? 3 : 4) void attend
   int page;
 
   RowState st;
-  frag q[4][N::kQ];
+  typename Q::frag q[4][N::kQ];
   {
     const int row = row_begin + x, i = row / a.group, hq = head * a.group + row % a.group;
     const bool on = row < rows;
@@ -129,9 +129,9 @@ __global__ __launch_bounds__(kWaves * 64, DT == SPINDLE_F32 ? 3 : 4) void attend
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub) {
         const u4 w = tile.k[sub * 2 + (k >> 1)];
-        const frag kk = N::template codes<FMT>(w[2 * (k & 1)], w[2 * (k & 1) + 1]);
+        const typename Q::frag kk = Q::template codes<FMT>(w[2 * (k & 1)], w[2 * (k & 1) + 1]);
 #pragma unroll
-        for (int part = N::kQ - 1; part >= 0; --part) s[sub] = N::mma(kk, q[k][part], s[sub]);
+        for (int part = N::kQ - 1; part >= 0; --part) s[sub] = Q::mma(kk, q[k][part], s[sub]);
       }
     const float f = fmaxf(factor * tile.ks, kTinyScale), slope = logit_slope<kMode>(f, a), offset = logit_offset<kMode>(a);
     float w[8];
@@ -146,8 +146,8 @@ __global__ __launch_bounds__(kWaves * 64, DT == SPINDLE_F32 ? 3 : 4) void attend
 #pragma unroll
     for (int j = 1; j < 8; ++j) top = larger(top, w[j]);
     bool scaled;
-    float back = gather<DT>(st, __builtin_fmaf(over_groups_max(top), slope, offset), &scaled);
-    const float base = offset - (st.m == -INFINITY ? 0.f : st.m - N::kLift);
+    float back = gather(st, __builtin_fmaf(over_groups_max(top), slope, offset), &scaled);
+    const float base = offset - (st.m == -INFINITY ? 0.f : st.m);
     // V's scale counts against the largest one so far
     float vf = 1.f;
     if (tile.vs > ref) {
@@ -163,8 +163,8 @@ __global__ __launch_bounds__(kWaves * 64, DT == SPINDLE_F32 ? 3 : 4) void attend
       st.l += w[j];
       w[j] *= vf;
     }
-    frag p[N::kP];
-    N::template split<N::kP>(w, p);
+    Weights::frag p[N::kP];
+    Weights::split<N::kP>(w, p);
     if (scaled) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) o[i] *= back;
@@ -183,9 +183,9 @@ __global__ __launch_bounds__(kWaves * 64, DT == SPINDLE_F32 ? 3 : 4) void attend
         transpose4(tile.v[4 * h][lo], tile.v[4 * h + 1][lo], tile.v[4 * h + 2][lo], tile.v[4 * h + 3][lo], &col[h][4 * lo]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const frag vv = N::template codes<FMT>(col[0][i], col[1][i]);
+      const Weights::frag vv = Weights::codes<FMT>(col[0][i], col[1][i]);
 #pragma unroll
-      for (int part = N::kP - 1; part >= 0; --part) o[i] = N::mma(vv, p[part], o[i]);
+      for (int part = N::kP - 1; part >= 0; --part) o[i] = Weights::mma(vv, p[part], o[i]);
     }
   };
   constexpr int kStride = kWaves * kTile;
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(kWaves * 64, DT == SPINDLE_F32 ? 3 : 4) void attend
 #pragma unroll
     for (int j = 0; j < 8; ++j) e[j] = Elem<DT>::from_float(res[j]);
     __builtin_memcpy(__builtin_assume_aligned(a.out + (at * kHeadDim + d) * sizeof(T), 16), e, sizeof(e));
-    if (a.lse && d == 0) a.lse[at] = lse_of<DT>(top, sum);
+    if (a.lse && d == 0) a.lse[at] = lse_of(top, sum);
   } else {
     float *po = a.part_o + (at * a.splits + split) * kHeadDim + d;
     *reinterpret_cast<f4 *>(po) = f4{res[0], res[1], res[2], res[3]};
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(32 * kJoinGroups) void attend_join(AttendArgs a) {
   typename Elem<DT>::type *out = reinterpret_cast<typename Elem<DT>::type *>(a.out) + at * kHeadDim + 4 * d;
 #pragma unroll
   for (int j = 0; j < 4; ++j) out[j] = Elem<DT>::from_float(v[j] * inv);
-  if (a.lse && d == 0) a.lse[at] = lse_of<DT>(top, sum);
+  if (a.lse && d == 0) a.lse[at] = lse_of(top, sum);
 }
 
 // The same for rows of few chunks: 32 threads per row, sixteen rows to a workgroup.
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(32 * kJoinGroups) void attend_join_few(AttendArgs a
 #pragma unroll
   for (int j = 0; j < 4; ++j) e[j] = Elem<DT>::from_float(v[j] * inv);
   __builtin_memcpy(__builtin_assume_aligned(reinterpret_cast<typename Elem<DT>::type *>(a.out) + at * kHeadDim + 4 * d, 8), e, sizeof(e));
-  if (a.lse && d == 0) a.lse[at] = lse_of<DT>(top, sum);
+  if (a.lse && d == 0) a.lse[at] = lse_of(top, sum);
 }
 
 // Waves of a workgroup: many where one workgroup takes a whole context, without a second kernel.

@@ -10,7 +10,7 @@ constexpr int kFrag = 1024;                      // bytes of an operand of one w
 constexpr int kBuffer = 16 * kFrag;              // K or V of a step as operands
 
 // One workgroup attends 128 rows over one chunk: a wave has 32 rows of its own, and all four share the step's tokens.
-// Codes become f16 or bf16 once for all of them, on their way into LDS, in the order in which the matrix instructions
+// Codes become operands once for all of them, on their way into LDS, in the order in which the matrix instructions
 // take them (V is turned on the way); a wave would otherwise spend as many vector instructions on unpacking as on the
 // softmax of its rows.  Two buffers: while one step is computed the next one is unpacked and the one after it is on its way,
 // with one barrier a step.  Two workgroups share a compute unit, so that one's products run beside the other's softmax.
@@ -28,7 +28,8 @@ template <int DT, int FMT, int kMode>
 __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
   typedef typename Elem<DT>::type T;
   typedef Num<DT> N;
-  typedef typename N::frag frag;
+  typedef typename N::Q Q;
+  typedef Weights::frag frag;
   extern __shared__ char lds[];                  // [2][K: half 2 x step 8][64 lanes][16 bytes], [2][V: step 4 x tile 4][64][16]
   const CacheView &c = a.c;
   const int tid = threadIdx.x, lane = lane_id(), x = lane & 31, g = lane >> 5;
@@ -56,7 +57,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
   const bool idle = wave_row >= rows;            // nothing to attend, but its share of the tokens to unpack
   const int least = limit_of(min(wave_row, rows - 1));
   RowState st;
-  frag q[8][1];
+  typename Q::frag q[8][1];
   const int row = wave_row + x;
   const bool on = row < rows;
   {
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
   // E4M3's scales are powers of two and go into V's bf16 operands for nothing (of a scale that is none, from a pool that was
   // filled elsewhere, what is left over goes into the weights).  Other operands are the codes, counting `ref` (the
   // largest scale so far) each, and the weights are multiplied.
-  constexpr bool kTrueV = FMT == SPINDLE_E4M3 && DT == SPINDLE_BF16;
+  constexpr bool kTrueV = FMT == SPINDLE_E4M3;
   float ref = kTrueV ? 1.f : kTinyScale;
 
   f16v o[4], s[2];                                // [32 dimensions][..], [32 tokens][..]; the row is lane % 32
@@ -130,8 +131,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
     for (int h = 0; h < 2; ++h) {
       asm volatile("" : "+v"(raw_k[h]));
       char *const to = k_to + buffer * kBuffer + h * (8 * kFrag);
-      *reinterpret_cast<frag *>(to) = N::template codes<FMT>(raw_k[h][0], raw_k[h][1]);
-      *reinterpret_cast<frag *>(to + 512) = N::template codes<FMT>(raw_k[h][2], raw_k[h][3]);
+      *reinterpret_cast<typename Q::frag *>(to) = Q::template codes<FMT>(raw_k[h][0], raw_k[h][1]);
+      *reinterpret_cast<typename Q::frag *>(to + 512) = Q::template codes<FMT>(raw_k[h][2], raw_k[h][3]);
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -145,7 +146,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
       char *const to = v_to + buffer * kBuffer + h * (8 * kFrag);
 #pragma unroll
       for (int e = 0; e < 4; e += 2) {           // (8 bytes of each of two dimensions at a time)
-        const u4 w = __builtin_bit_cast(u4, N::template codes<FMT>(col[e], col[e + 1], kTrueV && next[h].there ? power_of(next[h].vs) : 1.f));
+        const u4 w = __builtin_bit_cast(u4, Weights::codes<FMT>(col[e], col[e + 1], kTrueV && next[h].there ? power_of(next[h].vs) : 1.f));
         *reinterpret_cast<u2 *>(to + ((v_lane0 + e) ^ v_turn) * 16) = u2{w[0], w[1]};
         *reinterpret_cast<u2 *>(to + ((v_lane0 + e + 1) ^ v_turn) * 16) = u2{w[2], w[3]};
       }
@@ -173,7 +174,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
 #pragma unroll
       for (int part = N::kP - 1; part >= 0; --part)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = N::mma32(vv[i], p[u][part], o[i]);
+        for (int i = 0; i < 4; ++i) o[i] = Weights::mma32(vv[i], p[u][part], o[i]);
     }
   };
   __syncthreads();
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
 #pragma unroll
       for (int k = 0; k < 8; ++k)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) s[h] = N::mma32(*reinterpret_cast<const frag *>(from + (h * 8 + k) * kFrag), q[k][0], k ? s[h] : zero);
+        for (int h = 0; h < 2; ++h) s[h] = Q::mma32(*reinterpret_cast<const typename Q::frag *>(from + (h * 8 + k) * kFrag), q[k][0], k ? s[h] : zero);
     }
     unpack(t + stride, (n + 1) & 1);
     const Place here[2] = {now[0], now[1]};
@@ -266,9 +267,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
 #pragma unroll
       for (int e = 1; e < 16; ++e) top[0] = larger(top[0], s[0][e]), top[1] = larger(top[1], s[1][e]);
       bool more;
-      const float back = gather<DT>(st, over_halves_max(larger(__builtin_fmaf(top[0], slope[0], offset), __builtin_fmaf(top[1], slope[1], offset))), &more) * vback;
+      const float back = gather(st, over_halves_max(larger(__builtin_fmaf(top[0], slope[0], offset), __builtin_fmaf(top[1], slope[1], offset))), &more) * vback;
       scaled |= more;
-      const float base = offset - (st.m == -INFINITY ? 0.f : st.m - N::kLift);
+      const float base = offset - (st.m == -INFINITY ? 0.f : st.m);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const float from = base + log_v[u >> 1];
@@ -283,7 +284,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) w[j] *= rest_v[u >> 1];
         }
-        N::template split<N::kP>(w, p[u]);
+        Weights::split<N::kP>(w, p[u]);
       }
       if (scaled) {
 #pragma unroll
@@ -309,7 +310,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
         for (int j = 0; j < 4; ++j) e[j] = Elem<DT>::from_float(o[i][4 * k + j] * inv);
         __builtin_memcpy(__builtin_assume_aligned(a.out + (out_row * kHeadDim + 32 * i + 8 * k + 4 * g) * sizeof(T), 8), e, sizeof(e));
       }
-    if (a.lse && g == 0) a.lse[out_row] = lse_of<DT>(st.m, l);
+    if (a.lse && g == 0) a.lse[out_row] = lse_of(st.m, l);
   } else {
     float *po = a.part_o + (out_row * a.splits + split) * kHeadDim + 4 * g;
 #pragma unroll

@@ -74,12 +74,12 @@ struct Code<SPINDLE_E4M3> {
   static __device__ __forceinline__ float magnitude(uint32_t key) {
     return __builtin_amdgcn_cvt_pk_f32_fp8((int)key, false)[0];
   }
-  // four codes times a power of two as f16 (exact within its range), two pairs
-  static __device__ __forceinline__ void to_half(uint32_t w, float scale, h2 *lo, h2 *hi) {
-    *lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, false);
-    *hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, true);
+  // four codes as f16, two pairs
+  static __device__ __forceinline__ void to_half(uint32_t w, h2 *lo, h2 *hi) {
+    *lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false);
+    *hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true);
   }
-  // the same as bf16, in two words
+  // four codes times a power of two as bf16 (exact within its range), in two words
   static __device__ __forceinline__ void to_bf16(uint32_t w, float scale, uint32_t *out) {
     out[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
     out[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true));
@@ -128,7 +128,7 @@ struct Code<SPINDLE_I8> {
   static __device__ __forceinline__ float magnitude(uint32_t key) { return (float)key; }
   // as they are (their scales are no powers of two, a product would be rounded): 0x6400 | (c + 128) is the f16 number
   // 1024 + c + 128
-  static __device__ __forceinline__ void to_half(uint32_t w, float, h2 *lo, h2 *hi) {
+  static __device__ __forceinline__ void to_half(uint32_t w, h2 *lo, h2 *hi) {
     w ^= 0x80808080u;
     const h2 off = {(_Float16)-1152.f, (_Float16)-1152.f};
     *lo = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u)) + off;

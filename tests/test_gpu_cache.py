@@ -727,3 +727,65 @@ def test_attend_scales_that_are_no_powers_of_two(sb, dtype):
     cache.k_scale.fill_(1.5)
     got, _ = check_attend(sb, rng, cache, table, lens, [40, 25], 4, dtype)
     assert torch.isfinite(got.float()).all()
+
+
+@pytest.mark.parametrize("new", [3, 40])
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("dtype", list(DT))
+def test_attend_beside_a_page_of_far_larger_values_that_gets_no_weight(sb, dtype, fmt, new):
+    """The first page's V is some 10^9 times the others', and a bias by distance leaves it nothing: what the others give keeps its
+    bits."""
+    rng = np.random.default_rng(103)
+    n = 320
+    K, V = tokens(rng, n, 2), tokens(rng, n, 2)
+    V[:64] *= np.float32(2e9)
+    cache = sb.new_cache(6, 2, 64, fmt)
+    table = np.int32([[3, 0, 4, 1, 5]])
+    sb.cache_append(cache, dev(table), dev(np.int32([0])), dev(K), dev(V), cu_new=dev(np.int32([0, n])), max_new=n)
+    check_attend(sb, rng, cache, table, [n], [new], 4, dtype, slopes=np.full(8, 0.5, np.float32))
+    # the same within one step of 64 tokens: the second page of 32 gets nearly all the weight
+    V = tokens(rng, n, 2)
+    V[:32] *= np.float32(2e9)
+    cache = sb.new_cache(12, 2, 32, fmt)
+    table = table_of(rng, [10], 10, 12)
+    sb.cache_append(cache, dev(table), dev(np.int32([0])), dev(K), dev(V), cu_new=dev(np.int32([0, n])), max_new=n)
+    check_attend(sb, rng, cache, table, [n], [new], 4, dtype, slopes=np.full(8, 2, np.float32), q_pos=np.full(new, 63))
+
+
+@pytest.mark.parametrize("new", [2, 40])
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("dtype", list(DT))
+def test_attend_weights_hold_their_bits(sb, dtype, fmt, new):
+    """Two tokens of opposite V and nearly equal weights: the output is the difference of the weights, where their own rounding
+    is not hidden by the output's.  16-bit queries: two bf16, half a step of the second is 2^-16 of a weight; f32: three, whose
+    rounding is behind that of the sums.  In f32 and relative to the weights: 3 x 128 products of a logit (2^-23 of their size
+    each, matrix instructions may cut off), two logits; exponential, factors, sums and quotient some 2^-23 each, 2^-20 in all."""
+    rng = np.random.default_rng(107)
+    K, V = tokens(rng, 2, 2), tokens(rng, 2, 2)
+    V[1] = -V[0]
+    cache = sb.new_cache(2, 2, 32, fmt)
+    table, lens, cu = np.int32([[1]]), np.int32([2]), np.int32([0, new])
+    sb.cache_append(cache, dev(table), dev(np.int32([0])), dev(K), dev(V), cu_new=dev(np.int32([0, 2])), max_new=2)
+    Q = torch.from_numpy((1e-3 * rng.standard_normal((new, 8, 128))).astype(np.float32)).to(DT[dtype])
+    got = sb.cache_attend(cache, dev(table), dev(lens), Q.cuda(), 4, cu_q=dev(cu), max_q=new, prefix=dev(np.int32([2])))
+    want, _, size, big = ref.attend(pools_of(cache), table, lens, Q.double().numpy(), cu, 4, 128 ** -0.5, prefix=[2])
+
+    def bound(bits):
+        rounding = np.abs(want) * float(torch.finfo(DT[dtype]).eps) / 2 + (2.0 ** -25 if dtype == "f16" else 1e-30)
+        return size * (bits + 2 * 384 * 2.0 ** -23 * big[..., None] + 2.0 ** -20) + rounding
+
+    tol = bound(0.0 if dtype == "f32" else 2.0 ** -16)
+    worst = (np.abs(got.double().cpu().numpy() - want) / tol).max()
+    assert worst <= 1, f"{worst} times the bound"
+    # the bound tells one operand less apart: weights p and 1 - p of V and -V, the larger one counted as 1
+    x = pools_of(cache)
+    v = np.repeat(x.x[1][1, :, 0] * x.s[1][1, :, None], 4, axis=0)
+    less = np.zeros_like(want)
+    for i in range(new):
+        for h in range(8):
+            p = np.clip((1 + want[i, h, np.abs(v[h]).argmax()] / v[h][np.abs(v[h]).argmax()]) / 2, 0, 1)
+            w = np.array([p, 1 - p]) / max(p, 1 - p)
+            step = 2.0 ** np.floor(np.log2(w)) * (2.0 ** -7 if dtype != "f32" else 2.0 ** -15)
+            w = np.rint(w / step) * step
+            less[i, h] = v[h] * (w[0] - w[1]) * max(p, 1 - p)
+    assert (np.abs(less - want) > tol).any()
