@@ -80,7 +80,7 @@ struct Num<SPINDLE_F16> {
 typedef Bf16Operand Weights;                     // of the weights and V
 
 // A row's weights are counted from a logit that its largest one may exceed by so much (log2) before what was gathered is
-// scaled down.
+// scaled down; they are lowered by as much, so that none is above 1 and its product with V is no larger than V.
 constexpr float kSlack = 8.f;
 
 struct AttendArgs {
@@ -149,7 +149,7 @@ __device__ __forceinline__ float over_groups_sum(float v) {
 
 // log sum exp of a row from its reference logit (log2) and sum; a row that sees nothing has -inf, NaN stays.
 __device__ __forceinline__ float lse_of(float top, float sum) {
-  return sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) / kLog2e : sum == sum ? -INFINITY : sum;
+  return sum > 0.f ? (top + kSlack + __builtin_amdgcn_logf(sum)) / kLog2e : sum == sum ? -INFINITY : sum;
 }
 
 // What a row of the tile is, and what it has gathered so far.

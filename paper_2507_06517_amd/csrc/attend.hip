@@ -119,7 +119,6 @@ __global__ __launch_bounds__(kWaves * 64, DT == SPINDLE_F32 ? 3 : 4) void attend
   f4 o[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) o[i] = f4{0, 0, 0, 0};
-  float ref = kTinyScale;                                           // V's codes count ref each in o
 
   auto step = [&](int t) {
     tile.hold_k();
@@ -146,22 +145,15 @@ __global__ __launch_bounds__(kWaves * 64, DT == SPINDLE_F32 ? 3 : 4) void attend
 #pragma unroll
     for (int j = 1; j < 8; ++j) top = larger(top, w[j]);
     bool scaled;
-    float back = gather(st, __builtin_fmaf(over_groups_max(top), slope, offset), &scaled);
-    const float base = offset - (st.m == -INFINITY ? 0.f : st.m);
-    // V's scale counts against the largest one so far
-    float vf = 1.f;
-    if (tile.vs > ref) {
-      back *= ref * __builtin_amdgcn_rcpf(tile.vs);
-      ref = tile.vs;
-      scaled = true;
-    } else {
-      vf = tile.vs * __builtin_amdgcn_rcpf(ref);
-    }
+    const float back = gather(st, __builtin_fmaf(over_groups_max(top), slope, offset), &scaled);
+    const float base = offset - (st.m == -INFINITY ? 0.f : st.m + kSlack);
+    // V's scale goes into the weights, but for an E4M3 scale's power of two, which goes into the operands
+    const float v_scale = FMT == SPINDLE_E4M3 ? operand_scale(tile.vs) : 1.f, v_rest = tile.vs * (1.f / v_scale);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(w[j], slope, base));
       st.l += w[j];
-      w[j] *= vf;
+      w[j] *= v_rest;
     }
     Weights::frag p[N::kP];
     Weights::split<N::kP>(w, p);
@@ -183,7 +175,7 @@ __global__ __launch_bounds__(kWaves * 64, DT == SPINDLE_F32 ? 3 : 4) void attend
         transpose4(tile.v[4 * h][lo], tile.v[4 * h + 1][lo], tile.v[4 * h + 2][lo], tile.v[4 * h + 3][lo], &col[h][4 * lo]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const Weights::frag vv = Weights::codes<FMT>(col[0][i], col[1][i]);
+      const Weights::frag vv = Weights::codes<FMT>(col[0][i], col[1][i], v_scale);
 #pragma unroll
       for (int part = N::kP - 1; part >= 0; --part) o[i] = Weights::mma(vv, p[part], o[i]);
     }
@@ -202,7 +194,7 @@ __global__ __launch_bounds__(kWaves * 64, DT == SPINDLE_F32 ? 3 : 4) void attend
   __shared__ float so[kWaves][kRows][kHeadDim + 4];
   __shared__ float2 sml[kWaves][kRows];
   const float l = over_groups_sum(st.l);
-  const float inv = l > 0.f ? ref / l : l;                          // a row that saw nothing: 0; NaN stays
+  const float inv = l > 0.f ? 1.f / l : l;                          // a row that saw nothing: 0; NaN stays
 #pragma unroll
   for (int e = 0; e < 4; ++e)
 #pragma unroll

@@ -71,10 +71,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
   }
   const float factor = kMode == kPlain ? a.scale * kLog2e : a.scale;
   // E4M3's scales are powers of two and go into V's bf16 operands for nothing (of a scale that is none, from a pool that was
-  // filled elsewhere, what is left over goes into the weights).  Other operands are the codes, counting `ref` (the
-  // largest scale so far) each, and the weights are multiplied.
+  // filled elsewhere, what is left over goes into the weights).  Integers are the codes, and the weights are multiplied.
   constexpr bool kTrueV = FMT == SPINDLE_E4M3;
-  float ref = kTrueV ? 1.f : kTinyScale;
 
   f16v o[4], s[2];                                // [32 dimensions][..], [32 tokens][..]; the row is lane % 32
   frag p[4][N::kP];                              // weights of 16 tokens
@@ -146,7 +144,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
       char *const to = v_to + buffer * kBuffer + h * (8 * kFrag);
 #pragma unroll
       for (int e = 0; e < 4; e += 2) {           // (8 bytes of each of two dimensions at a time)
-        const u4 w = __builtin_bit_cast(u4, Weights::codes<FMT>(col[e], col[e + 1], kTrueV && next[h].there ? power_of(next[h].vs) : 1.f));
+        const u4 w = __builtin_bit_cast(u4, Weights::codes<FMT>(col[e], col[e + 1], kTrueV && next[h].there ? operand_scale(next[h].vs) : 1.f));
         *reinterpret_cast<u2 *>(to + ((v_lane0 + e) ^ v_turn) * 16) = u2{w[0], w[1]};
         *reinterpret_cast<u2 *>(to + ((v_lane0 + e + 1) ^ v_turn) * 16) = u2{w[2], w[3]};
       }
@@ -207,27 +205,21 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
       const bool there[2] = {here[0].there, here[1].there};
       const float kf[2] = {there[0] ? fmaxf(factor * here[0].ks, kTinyScale) : 1.f, there[1] ? fmaxf(factor * here[1].ks, kTinyScale) : 1.f};
       const float slope[2] = {logit_slope<kMode>(kf[0], a), logit_slope<kMode>(kf[1], a)}, offset = logit_offset<kMode>(a);
-      // V's scale against the largest one so far goes into the exponent, and out of the sum again; what is far under it
-      // (2^-60) is multiplied in at the end, where the sum cannot lose it
-      float log_v[2] = {0.f, 0.f}, per_v[2] = {1.f, 1.f}, rest_v[2] = {1.f, 1.f}, vback = 1.f;
-      bool scaled = false, tiny_v = false;
-      const bool odd_v = kTrueV && ((__float_as_uint(here[0].vs) | __float_as_uint(here[1].vs)) & 0x7FFFFFu) != 0;
+      // an integer's V scale goes into the exponent, and out of the sum again; what is far from 1 is multiplied in at the end,
+      // where neither the exponent's bits nor the sum can suffer
+      float log_v[2] = {0.f, 0.f}, per_v[2] = {1.f, 1.f}, rest_v[2] = {1.f, 1.f};
+      const bool odd_v = kTrueV && (operand_scale(here[0].vs) != here[0].vs || operand_scale(here[1].vs) != here[1].vs);
+      bool far_v = false;
       if (!kTrueV) {
-        const float v[2] = {there[0] ? here[0].vs : 0.f, there[1] ? here[1].vs : 0.f};
-        const float was = ref;
-        ref = fmaxf(ref, fmaxf(v[0], v[1]));
-        const float inv = __builtin_amdgcn_rcpf(ref);
-        scaled = ref > was;
-        if (scaled) vback = was * inv;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float f = v[h] * inv;
-          if (f < 0x1p-60f) {
-            rest_v[h] = f;
-            tiny_v = true;
+          const float v = there[h] ? here[h].vs : 1.f, log = __builtin_amdgcn_logf(v);
+          if (__builtin_fabsf(log) <= 24.f) {
+            log_v[h] = log;
+            per_v[h] = __builtin_amdgcn_exp2f(-log);
           } else {
-            log_v[h] = __builtin_amdgcn_logf(f);
-            per_v[h] = __builtin_amdgcn_exp2f(-log_v[h]);
+            rest_v[h] = v;
+            far_v = true;
           }
         }
       }
@@ -253,7 +245,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (!there[h] || !(here[h].vs > 0.f)) continue;
-            log_v[h] = __builtin_amdgcn_logf(here[h].vs * (1.f / power_of(here[h].vs)));   // 0 of a power of two
+            log_v[h] = __builtin_amdgcn_logf(here[h].vs * (1.f / operand_scale(here[h].vs)));   // 0 of a power of two
             per_v[h] = __builtin_amdgcn_exp2f(-log_v[h]);
           }
         }
@@ -266,10 +258,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
       float top[2] = {s[0][0], s[1][0]};
 #pragma unroll
       for (int e = 1; e < 16; ++e) top[0] = larger(top[0], s[0][e]), top[1] = larger(top[1], s[1][e]);
-      bool more;
-      const float back = gather(st, over_halves_max(larger(__builtin_fmaf(top[0], slope[0], offset), __builtin_fmaf(top[1], slope[1], offset))), &more) * vback;
-      scaled |= more;
-      const float base = offset - (st.m == -INFINITY ? 0.f : st.m);
+      bool scaled;
+      const float back = gather(st, over_halves_max(larger(__builtin_fmaf(top[0], slope[0], offset), __builtin_fmaf(top[1], slope[1], offset))), &scaled);
+      const float base = offset - (st.m == -INFINITY ? 0.f : st.m + kSlack);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const float from = base + log_v[u >> 1];
@@ -280,7 +271,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
           sum += w[j];
         }
         st.l = __builtin_fmaf(sum, per_v[u >> 1], st.l);
-        if (!kTrueV && tiny_v) {
+        if (!kTrueV && far_v) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) w[j] *= rest_v[u >> 1];
         }
@@ -298,7 +289,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
   // dimension 32 i + 8 k + 4 g + e of row x is o[i][4 k + e]
   const float l = over_halves_sum(st.l);
   if (!on) return;
-  const float inv = l > 0.f ? ref / l : l;                          // a row that saw nothing: 0; NaN stays
+  const float inv = l > 0.f ? 1.f / l : l;                          // a row that saw nothing: 0; NaN stays
   const size_t out_row = (size_t)(t0 + row / a.group) * a.heads_q + head * a.group + row % a.group;
   if (a.splits == 1) {
 #pragma unroll

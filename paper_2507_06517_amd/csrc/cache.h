@@ -32,8 +32,11 @@ __device__ __forceinline__ uint64_t page_bytes(const CacheView &c, uint32_t numb
   return ((uint64_t)number << (c.shift + 7)) + ((uint32_t)slot << 7);
 }
 
-// The power of two that a scale is, or that lies below it: its exponent, for what takes nothing else (at least 2^-126).
-__device__ __forceinline__ float power_of(float scale) { return __uint_as_float(max(__float_as_uint(scale) & 0x7F800000u, 0x00800000u)); }
+// What of an E4M3 scale goes into a bf16 operand: the power of two that it is, or that lies below it, and no more than 2^100, where
+// no code becomes infinite.
+__device__ __forceinline__ float operand_scale(float scale) {
+  return __uint_as_float(min(max(__float_as_uint(scale) & 0x7F800000u, 0x00800000u), 0x71800000u));
+}
 
 template <int FMT>
 struct Code;

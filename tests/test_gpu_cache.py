@@ -789,3 +789,23 @@ def test_attend_weights_hold_their_bits(sb, dtype, fmt, new):
             w = np.rint(w / step) * step
             less[i, h] = v[h] * (w[0] - w[1]) * max(p, 1 - p)
     assert (np.abs(less - want) > tol).any()
+
+
+@pytest.mark.parametrize("new", [3, 40])
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("dtype", list(DT))
+def test_attend_largest_numbers_in_masked_places(sb, dtype, fmt, new):
+    """The last token's V holds the largest numbers; the rows before do not see it, whether they share a step with it or a wave
+    only."""
+    rng = np.random.default_rng(101)
+    n = 516
+    K, V = (dev(tokens(rng, n, 2)) for _ in range(2))
+    V[n - 1] = torch.finfo(torch.float32).max
+    cache = sb.new_cache(18, 2, 32, fmt)
+    table = table_of(rng, [17], 17, 18)
+    sb.cache_append(cache, dev(table), dev(np.int32([0])), K, V, cu_new=dev(np.int32([0, n])), max_new=n)
+    Q = torch.from_numpy(rng.standard_normal((new, 8, 128)).astype(np.float32)).to(DT[dtype])
+    cu = np.int32([0, new])
+    got, lse = sb.cache_attend(cache, dev(table), dev(np.int32([n])), Q.cuda(), 4, cu_q=dev(cu), max_q=new, want_lse=True)
+    want = ref.attend(pools_of(cache), table, [n], Q.double().numpy(), cu, 4, 128 ** -0.5)
+    compare_attend(got[:-1], lse[:-1], *(x[:-1] for x in want), n, dtype)
