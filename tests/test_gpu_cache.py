@@ -809,3 +809,68 @@ def test_attend_largest_numbers_in_masked_places(sb, dtype, fmt, new):
     got, lse = sb.cache_attend(cache, dev(table), dev(np.int32([n])), Q.cuda(), 4, cu_q=dev(cu), max_q=new, want_lse=True)
     want = ref.attend(pools_of(cache), table, [n], Q.double().numpy(), cu, 4, 128 ** -0.5)
     compare_attend(got[:-1], lse[:-1], *(x[:-1] for x in want), n, dtype)
+
+
+# ------------------------------------------------------------------ the kernel for many rows: what the tests above show with few
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_many_rows_with_positions_empty_slots_and_absent_pages(sb, dtype, fmt):
+    rng = np.random.default_rng(109)
+    lens, new = [0, 3, 170, 90, 300], [40, 45, 44, 50, 41]
+    cache, table = filled(sb, rng, lens, 2, 32, fmt, positions=True)
+    where = np.cumsum(rng.integers(1, 5, (cache.n_pages, 2, 32)), axis=2).astype(np.int32)   # gaps, other ones for each head
+    for b, n in enumerate(lens):
+        for j in range(-(-n // 32)):
+            cache.pos[int(table[b, j])] = dev(where[0] + 130 * j)
+    slopes, q_pos = np.float32(0.003 * np.arange(8)), rng.integers(0, 1500, sum(new))
+    check_attend(sb, rng, cache, table, lens, new, 4, dtype, slopes=slopes, q_pos=q_pos)
+    check_attend(sb, rng, cache, table, lens, new, 4, dtype, prefix=[5, 2, 0, 0, 290])
+    cache.pos[int(table[2, 0])] = -1                                 # slots without a token
+    cache.pos[int(table[2, 2]), 1, ::3] = -1
+    cache.pos[int(table[3, 0]), 1] = -7
+    cache.pos[int(table[4, 3]), 0, 5:] = -1
+    table[3, 1], table[3, 2], table[4, 8] = -1, cache.n_pages, -5
+    got, lse = check_attend(sb, rng, cache, table, lens, new, 4, dtype, slopes=slopes, q_pos=q_pos)
+    assert (got[:40] == 0).all() and torch.isneginf(lse[:40]).all()
+    check_attend(sb, rng, cache, table, lens, new, 4, dtype, softcap=6.0, q_scale=4.0)
+    # the same pages without positions
+    plain = sb.Cache(cache.k, cache.v, cache.k_scale, cache.v_scale, None, 32, fmt)
+    check_attend(sb, rng, plain, table, lens, new, 4, dtype)
+    check_attend(sb, rng, plain, table, lens, new, 4, dtype, softcap=6.0, prefix=[0, 3, 100, 90, 7])
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_many_rows_over_pages_of_very_different_scales(sb, dtype, fmt):
+    rng = np.random.default_rng(113)
+    for order in ([1, 1e-6, 1e4, 0, 1e-30], [1e4, 1, 1e-3, 1e-20, 0], [1e-30, 1e-20, 1e-3, 1, 30]):
+        x = np.concatenate([tokens(rng, 64, 1) * np.float32(f) for f in order])
+        k = np.concatenate([tokens(rng, 64, 1) * np.float32(min(f, 1.0)) for f in order])
+        if dtype == "f16":
+            x = np.clip(x, -6e4, 6e4)
+        cache = sb.new_cache(8, 1, 64, fmt)
+        table = np.int32([[3, 1, 4, 0, 6]])
+        sb.cache_append(cache, dev(table), dev(np.int32([0])), dev(k), dev(x), cu_new=dev(np.int32([0, 320])), max_new=320)
+        check_attend(sb, rng, cache, table, [320], [40], 4, dtype)
+        check_attend(sb, rng, cache, table, [320], [320], 4, dtype)   # rows that see one page only, or two
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_many_rows_heavy_queries(sb, dtype, fmt):
+    """One query's NaN or infinity stays in its own rows; large bf16 queries are no overflow."""
+    rng = np.random.default_rng(127)
+    cache, table = filled(sb, rng, [150], 1, 32, fmt)
+    t, n = dev(table), dev(np.int32([150]))
+    Q = torch.from_numpy(rng.standard_normal((1, 40, 4, 128)).astype(np.float32)).to(DT[dtype]).cuda()
+    want = sb.cache_attend(cache, t, n, Q, 4)
+    bad = Q.clone()
+    bad[0, 2, 1, 7], bad[0, 33, 2, 9] = float("nan"), float("inf")
+    got = sb.cache_attend(cache, t, n, bad, 4)
+    spoiled = torch.zeros(40, 4, dtype=torch.bool, device="cuda")
+    spoiled[2, 1] = spoiled[33, 2] = True
+    assert torch.equal(got[0][~spoiled], want[0][~spoiled])
+    assert torch.isnan(got[0, 2, 1]).all()
+    if dtype == "bf16":
+        assert torch.equal(sb.cache_attend(cache, t, n, Q * 2.0 ** 100, 4, scale=2.0 ** -100 * 128 ** -0.5), want)
