@@ -1,6 +1,8 @@
 // What the attention kernels over the paged cache share.
 #pragma once
 
+#include <float.h>
+
 #include "cache.h"
 
 namespace spindle {
@@ -195,7 +197,7 @@ __device__ __forceinline__ float wide_capped(float x, const AttendArgs &a) {
 template <int kMode>
 __device__ __forceinline__ float raw_logit(float s, float f, const AttendArgs &a, const RowState &st, int k_at) {
   if (kMode == kPlain) return s;
-  if (kMode == kCapped) return __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s * (f * a.cap_in)));
+  if (kMode == kCapped) return __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s * fminf(f * a.cap_in, FLT_MAX)));   // (0 * inf is none)
   float w = s * f;
   if (a.softcap > kWideCap) w = wide_capped(w, a) * kLog2e;
   else if (a.softcap > 0.f) w = a.cap_out + 2.f * a.cap_out * __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(w * a.cap_in));

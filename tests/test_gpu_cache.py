@@ -874,3 +874,22 @@ def test_many_rows_heavy_queries(sb, dtype, fmt):
     assert torch.isnan(got[0, 2, 1]).all()
     if dtype == "bf16":
         assert torch.equal(sb.cache_attend(cache, t, n, Q * 2.0 ** 100, 4, scale=2.0 ** -100 * 128 ** -0.5), want)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_attend_small_caps_over_large_keys(sb, dtype):
+    """A product of zero stays zero, however large the quotient of K's scale and the cap is."""
+    rng = np.random.default_rng(139)
+    n = 70
+    K, V = (dev(tokens(rng, n, 2)) for _ in range(2))
+    cache = sb.new_cache(3, 2, 32, "i8")
+    table = np.int32([[2, 0, 1]])
+    sb.cache_append(cache, dev(table), dev(np.int32([0])), K * 1e15, V, cu_new=dev(np.int32([0, n])), max_new=n)
+    for new in (3, 40):
+        Q = torch.from_numpy(rng.standard_normal((new, 8, 128)).astype(np.float32)).to(DT[dtype])
+        Q[::2] = 0
+        cu = np.int32([0, new])
+        got, lse = sb.cache_attend(cache, dev(table), dev(np.int32([n])), Q.cuda(), 4, cu_q=dev(cu), max_q=new, softcap=1e-30, want_lse=True)
+        # logits of at most 1e-30 are none
+        want = ref.attend(pools_of(cache), table, [n], Q.double().numpy() * 0, cu, 4, 128 ** -0.5)
+        compare_attend(got, lse, *want, n, dtype)
