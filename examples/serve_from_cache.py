@@ -79,7 +79,7 @@ def serve(prompt=4096, budget=1024, branches=4, steps=16, fmt="e4m3", seed=0):
     for step in range(steps):
         q, k, v = layer(x)
         at = torch.full((branches,), prompt + step, dtype=torch.int32, device="cuda")   # places in the text, not in the cache
-        longer, copies, _ = sb.pages_reserve(refs, table, lens, one, PAGE)
+        longer, copies, _ = sb.pages_reserve(refs, table, lens, one, PAGE)   # (the pool has pages for every step: no status to wait for)
         sb.cache_copy(cache, copies)
         sb.cache_append(cache, table, lens, k, v, cu_new=cu, max_new=1, positions=at)
         o = sb.cache_attend(cache, table, longer, q, G, cu_q=cu, max_q=1, q_pos=at)

@@ -492,11 +492,12 @@ spindle_status spindle_attend_workspace_bytes(const spindle_cache *cache, int32_
 
 /*
  * Attention of the newest tokens of every sequence over what it holds (they are stored already: len counts them).
- * The queries of sequence b, m = cu_q[b+1] - cu_q[b] (max_q without cu_q), are its tokens len[b] - m .. len[b] - 1.  A query
+ * The queries of sequence b, m = cu_q[b+1] - cu_q[b] (max_q without cu_q; no sequence may have more than max_q), are its tokens
+ * len[b] - m .. len[b] - 1.  Rows of out that are no sequence's, by cu_q, are not written.  A query
  * of token s sees the tokens t <= s, and t < prefix[b] whatever s is.  Per query head h of KV head h / group_size:
  *   logit = scale * q.k_t;  capped: softcap * tanh(logit / softcap) if softcap > 0;
  *   logit -= slopes[h] * |position of the query - position of t|;  out = sum softmax(logit)_t v_t;  lse = log sum exp(logit)
- * A query that sees nothing gets zeros and lse = -inf.
+ * A query that sees nothing gets zeros and lse = -inf.  Calls without queries (max_q or total_q 0) take no pointers to them.
  *
  *   Q            [total_q, n_kv_heads * group_size, 128] in `dtype`; stride_t, stride_h in elements, multiples of 8
  *   scale        > 0, normally 1/sqrt(128)

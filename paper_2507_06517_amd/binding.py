@@ -627,8 +627,8 @@ def _ints(t, name, shape, device):
 
 
 class Cache:
-    """The pools of one layer: k, v uint8 [n_pages, H, page_tokens, 128], k_scale, v_scale float32 [n_pages, H] and,
-    optionally, pos int32 [n_pages, H, page_tokens]; format "e4m3" or "i8"."""
+    """The pools of one layer: k, v uint8 [n_pages, H, page_tokens, 128], k_scale, v_scale float32 [n_pages, H], positive, and,
+    optionally, pos int32 [n_pages, H, page_tokens]; format "e4m3" or "i8".  A program makes one and keeps it."""
 
     def __init__(self, k, v, k_scale, v_scale, pos, page_tokens, format):
         if format not in _FMT:
@@ -774,7 +774,8 @@ def cache_attend(cache: Cache, table, lens, Q, group_size, cu_q=None, max_q=None
     """Attention of the newest tokens (stored already, lens [B] counts them) over their sequences.  Q [B, m, H * group, d]
     (the tokens of all sequences at one stride), or, with cu_q [B + 1] int32, [tokens of all, H * group, d] and max_q, the most tokens
     of one sequence.  Returns out, or (out, lse) with want_lse; out, lse and
-    workspace may be passed in (a workspace of spindle_attend_workspace_bytes)."""
+    workspace may be passed in (a workspace of spindle_attend_workspace_bytes,
+    contiguous).  Rows of Q that are no sequence's, by cu_q, get nothing."""
     B, width = _check_table(cache, table, lens)
     dev, hq, shape, strides = cache.device, cache.n_kv_heads * group_size, Q.shape, Q.stride()
     if len(shape) != (4 if cu_q is None else 3) or shape[-1] != HEAD_DIM or shape[-2] != hq or strides[-1] != 1 or Q.device != dev:

@@ -61,11 +61,15 @@ struct Tile {
 // statistics are found by two lane exchanges.  Codes go from memory to registers in 16-byte (K) and 8-byte (V) pieces of whole
 // rows and never through LDS: a wave's 32 x 8 bytes of V are turned by 32 byte permutes, which the memory leaves time for.
 //
-// Bound by memory.  One token of 131071 (f16, E4M3, 268 MB): 41 us, 6.5 TB/s with part of it from the last-level cache, 4.5 with
-// nothing cached (58 us with the join); a large copy reaches 4.8.  32 ragged sequences (bf16, integers, 136 MB): 35 us, of which
-// a workgroup's start and end (three trips to memory, the join of the waves) are 5.  Four waves on a SIMD hide the trips better
-// than two or three with a tile in flight ahead (35 and 39 us); two row tiles a wave share what is unpacked and were slower
-// (drafted tokens 20 and 25 us).  1024 or 4096 workgroups instead of 2048: 62 and 42 against 39 us with the join.
+// Bound by memory where contexts are long.  One token of 131071 (f16, E4M3, 268 MB): 42 us, 6.4 TB/s with part of it from the
+// last-level cache, 4.6 with nothing cached (58 us with the join); a large copy reaches 4.9.  32 ragged sequences (bf16, integers,
+// 136 MB): 35 us, of which a workgroup's start and end (three trips to memory, the join of the waves) are 5.  Four waves on a SIMD
+// hide the trips better than two or three with a tile in flight ahead (35 and 39 us); two row tiles a wave share what is unpacked
+// and were slower (drafted tokens 20 and 25 us).  1024 or 4096 workgroups instead of 2048: 62 and 42 against 39 us with the join.
+// Short contexts are bound by the trips that wait for each other (drafted f32 tokens over 1000 to 2055: 19 us, vector
+// instructions busy for 28 % of it, matrix instructions for 7: two steps a wave between those trips and the join).
+// The biased forms have 4 to 7 registers more than four waves leave (f32: one more than three do), which spill: 32 ragged sequences
+// with stored positions 46 us, 38 without; three waves a SIMD hold them and take 48.
 template <int DT, int FMT, int kMode, int kWaves>
 __global__ __launch_bounds__(kWaves * 64, DT == SPINDLE_F32 ? 3 : 4) void attend(AttendArgs a) {
   typedef typename Elem<DT>::type T;
@@ -347,10 +351,10 @@ __global__ __launch_bounds__(32 * kJoinGroups) void attend_join_few(AttendArgs a
 constexpr int kFewWaves = 4, kManyWaves = 8, kTarget = 2048;
 
 // Many waves pay while the workgroups all run at once, two on a compute unit and one of f32, which has more registers (f16, bf16
-// integers and f32, contexts of 300: 256 workgroups 10.4, 10.2 and 10.2 us and few waves 13.1, 15.1 and 15.4; 800: 17.8, 22.1
-// and 27.0 us and 15.3, 18.6 and 18.9), and until the chunks of few waves make up for the launch of their join: 8 workgroups with
-// contexts of 1000 10.8, 12.9 and 12.4 us (13.8, 15.5 and 15.0), of 2000 15.3, 19.6 and 18.4 (13.5, 15.5 and 14.8); with 160
-// workgroups, which leave the chunks less of the chip, of 2000 17.2, 22.3 and 21.4 us (21.6, 24.7 and 24.7).
+// integers and f32, contexts of 300: 256 workgroups 12.1, 11.4 and 11.1 us and few waves 16.3, 16.3 and 15.5; 800: 17.9, 22.3
+// and 27.4 us and 15.9, 18.5 and 19.3), and until the chunks of few waves make up for the launch of their join: 8 workgroups with
+// contexts of 1000 11.3, 13.3 and 13.3 us (15.7, 15.6 and 15.5), of 2000 15.9, 19.7 and 19.1 (16.1, 15.9 and 15.5); with 160
+// workgroups, which leave the chunks less of the chip, of 2000 18.0, 22.4 and 21.9 us (21.5, 23.3 and 23.2).
 bool many_waves(int64_t units, int64_t tokens, int dtype) {
   return units <= (dtype == SPINDLE_F32 ? 256 : 512) && tokens <= (units < 128 ? 1280 : 2048);
 }
@@ -367,8 +371,8 @@ Plan plan_attend(const CacheView &c, int batch, int width, int max_q, int total_
   Plan p;
   const int64_t rows = (int64_t)max_q * group, tokens = (int64_t)width * c.P;
   int64_t splits = 1;
-  // Rows of 16-bit queries share unpacked tokens from the fifth 16-row tile on (6 x 8 heads, 2000 tokens: 64 rows 23 us here and
-  // 27 there, 128 rows 36 and 31).
+  // Rows of 16-bit queries share unpacked tokens from the fifth 16-row tile on (6 x 8 heads, f16, integers, 2000 tokens: 64 rows
+  // 28 us here and 31 there, 128 rows 38 and 36, 256 rows 56 and 47).
   p.rows = rows > 64 && dtype != SPINDLE_F32;
   if (p.rows) {
     // What a cut takes, in microseconds: a step of 64 tokens 1.9 while every compute unit has one workgroup, 3 with two, which is

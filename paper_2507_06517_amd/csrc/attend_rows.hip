@@ -16,14 +16,15 @@ constexpr int kBuffer = 16 * kFrag;              // K or V of a step as operands
 // with one barrier a step.  Two workgroups share a compute unit, so that one's products run beside the other's softmax.
 //
 // Bound by the matrix and vector instructions together, and by the clock that falls with them: 2048 bf16 queries of 4 x 8 heads
-// over 16 Ki tokens take 0.74 to 0.80 ms, 0.59 with operands of zeros.  The products are 0.515 TFLOP, 0.43 ms at what a library
+// over 16 Ki tokens take 0.71 to 0.79 ms, 0.60 with operands of zeros.  The products are 0.515 TFLOP, 0.43 ms at what a library
 // product of 8192^3 reaches here (1.2 PFLOP/s), and 0.77 TFLOP with the second bf16 half of the weights, 0.64 ms.  Matrix
-// instructions are busy for 50 % of the cycles, vector instructions for 53.  Tried, at 0.80 for this form: eight waves of which four
+// instructions are busy for 49 % of the cycles, vector instructions for 54.  Tried, at 0.80 for this form: eight waves of which four
 // are half a step behind (0.77, but 90 us against 73 for five short f16 prompts with capped scores), eight in step (0.80, 97),
 // 16x16 products (0.79), V's products a step late (0.87), raised wave priority for products (0.86), forced interleaving (0.81).
-// Capped scores are bound by the vector instructions (three of a step's exponentials and reciprocals per logit), and so are
-// biased ones: the same 2048 queries with slopes and stored positions 1.06 ms (1.13 with one loop for stored and plain positions,
-// whose registers spill; 1.20 with a load for each position).
+// Slopes and stored positions add vector instructions: the same 2048 queries 1.05 ms (1.13 with one loop for stored and plain
+// positions, whose registers spill; 1.20 with a load for each position).  Short prompts are bound by the chain of the longest row
+// tile: five f16 prompts of 200 to 1500 tokens with capped scores take 66 us, in which 400 workgroups of up to 24 steps run all at
+// once and no unit is busy (vector instructions 28 %, matrix instructions 13, LDS 11).
 template <int DT, int FMT, int kMode>
 __global__ __launch_bounds__(kThreads, 2) void attend_rows(AttendArgs a) {
   typedef typename Elem<DT>::type T;
