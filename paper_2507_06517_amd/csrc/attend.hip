@@ -67,7 +67,7 @@ struct Tile {
 // hide the trips better than two or three with a tile in flight ahead (35 and 39 us); two row tiles a wave share what is unpacked
 // and were slower (drafted tokens 20 and 25 us).  1024 or 4096 workgroups instead of 2048: 62 and 42 against 39 us with the join.
 // Short contexts are bound by the trips that wait for each other (drafted f32 tokens over 1000 to 2055: 19 us, vector
-// instructions busy for 28 % of it, matrix instructions for 7: two steps a wave between those trips and the join).
+// instructions busy for 28 % of it, matrix instructions for 6: two steps a wave between those trips and the join).
 // The biased forms have 4 to 7 registers more than four waves leave (f32: one more than three do), which spill: 32 ragged sequences
 // with stored positions 46 us, 38 without; three waves a SIMD hold them and take 48.
 template <int DT, int FMT, int kMode, int kWaves>
